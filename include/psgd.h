@@ -323,6 +323,114 @@ PSGD_API psgd_status psgd_random_k_step(psgd_plan* plan, const void* grad, float
  * (-1 and 0 for vector tensors).  Either output may be NULL. */
 PSGD_API psgd_status psgd_plan_kept(const psgd_plan* plan, int32_t tensor, int64_t* kept_off, int64_t* kept);
 
+/* ---- The model's side of the step ---------------------------------------------------------------------------
+ *
+ * What produces the gradients that psgd_step compresses and reads the parameters that psgd_step_update steps, in
+ * the flat layout of the plan, and one more compressor for the same loop.  All take their random numbers from
+ * one counter-based generator (Philox4x32 with ten rounds; Salmon, Moraes, Dror, Shaw, 2011), so no mask is stored
+ * and no index buffer is needed: the backward pass draws again what the forward pass drew.
+ *
+ *   rng     (device, const)  two 64-bit words {seed, offset}, 8-byte aligned.  Key of the generator: the seed; upper
+ *                            half of its counter: the offset plus the argument `offset`.  A captured graph draws
+ *                            anew on each replay if the program moves rng[1] on between the replays; calls of one
+ *                            step are told apart by `offset`.  Same words, same offset: same mask.
+ *   p, drop                  drop probability in [0, 1], taken as the multiple d of 2^-16 next to it; the elements
+ *                            that stay are multiplied by 1 / (1 - d) (with d = 1 none does).  Element (row, col) of
+ *                            [rows][cols]: counter (col / 8, row), half word col % 8 of the four words (low
+ *                            half first), dropped where that is below 65536 d.  Strides do not matter.  A dropped
+ *                            element contributes exactly zero, also where it is infinite or NaN.  d = 0: rng may be
+ *                            NULL.
+ *
+ * Arithmetic is fp32 (bf16 data: bf16 operands, fp32 sums), rounded to the data type at the end; sums run in a fixed
+ * order, so results repeat bit for bit.  The calls only launch kernels on hip_stream: no allocation, no memset, no
+ * synchronisation (psgd_random_mask_step: after the plan's first GPU call), so they can be captured and replayed.
+ * Buffers are on the current device.  Strides are in elements between consecutive rows; 0 means packed rows. */
+
+typedef enum {
+    PSGD_ACT_IDENTITY = 0,
+    PSGD_ACT_RELU = 1,        /* max(z, 0); slope 0 at 0 */
+    PSGD_ACT_GELU = 2,        /* z (1 + erf(z / sqrt 2)) / 2 */
+    PSGD_ACT_GELU_TANH = 3,   /* z (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3))) / 2 */
+    PSGD_ACT_SILU = 4         /* z / (1 + exp(-z)) */
+} psgd_activation;
+
+/* A linear layer of the plan: matrix `weight` (rows = out features n, cols = in features k), vector `bias`. */
+typedef struct {
+    int32_t weight;          /* tensor index of a matrix of the plan */
+    int32_t bias;            /* tensor index of a vector of n elements, or -1 */
+    int32_t activation;      /* psgd_activation */
+    int32_t param_dtype;     /* type of `param`: PSGD_F32, or PSGD_BF16 on plans with bf16 gradients.  On those, fp32
+                                weights are rounded to bf16 (nearest even) as they enter the products; the bias is not */
+    int64_t tokens;          /* rows of x and y; 0 is allowed */
+    int64_t x_stride, residual_stride, pre_stride, y_stride;   /* forward; x_stride and pre_stride also backward */
+    int64_t dy_stride, dx_stride;                              /* backward */
+    double drop;             /* as above, of elements (token, out feature) */
+    const uint64_t* rng;
+    uint64_t offset;
+} psgd_linear;
+
+/* Scratch that psgd_linear_forward and psgd_linear_backward need for this layer and token count (the larger of the
+ * two; rng, drop and offset do not matter). */
+PSGD_API psgd_status psgd_linear_workspace(const psgd_plan* plan, const psgd_linear* op, int64_t* bytes);
+
+/* z = x W^T + b ; y = residual + D(act(z)).  x, residual, pre and y have the plan's grad_dtype.
+ *   param    (device, const)  flat parameters, laid out like `out` of psgd_decompress
+ *   x        (device, const)  [tokens][k]
+ *   residual (device, const)  [tokens][n] or NULL
+ *   pre      (device, out)    [tokens][n] or NULL: z, which the backward pass of an activation reads
+ *   y        (device, out)    [tokens][n]; may be `residual` itself with the same stride, otherwise outputs overlap
+ *                             nothing
+ *   workspace (device)        psgd_linear_workspace bytes, 256-byte aligned, contents ignored and left undefined;
+ *                             calls that may run at the same time need workspaces of their own
+ * Errors: PSGD_EINVAL for null or misaligned pointers, tensor indices that are not such a matrix or vector, a negative
+ * token count, a stride below the row length, drop outside [0, 1]; PSGD_EUNSUPPORTED for more than 2^20 rows or
+ * columns or a larger stride, more than 2^30 tokens, bf16 parameters on a plan with fp32 gradients. */
+PSGD_API psgd_status psgd_linear_forward(psgd_plan* plan, const psgd_linear* op, const void* param, const void* x,
+                                         const void* residual, void* pre, void* y, void* workspace, void* hip_stream);
+
+/* The gradients of that layer: dz = D(dy) act'(pre); dx = dz W; dW = dz^T x; db = sum over the tokens of dz (the
+ * residual's gradient is dy itself).  Where act' takes other values than 0 and 1, bf16 plans round dz to bf16 for the
+ * products; db is summed from the unrounded values.
+ *   pre      (device, const)  as stored by the forward pass; not read (may be NULL) with PSGD_ACT_IDENTITY
+ *   dy       (device, const)  [tokens][n]
+ *   dx       (device, out)    [tokens][k], or NULL: not computed (param may then be NULL)
+ *   grad     (device, in/out) [W][grad_stride], the gradients that psgd_step takes: dW and db are written at the
+ *                             tensors' places of worker `worker`, nothing else of it is touched; or NULL: not computed
+ *                             (x may then be NULL)
+ *   accumulate                1: dW and db are added to what grad holds (micro-batches, a weight used twice)
+ * tokens = 0: dW and db are set to zero unless accumulate.  Same errors; PSGD_EINVAL also for a worker outside
+ * [0, W) and for dx and grad both NULL. */
+PSGD_API psgd_status psgd_linear_backward(psgd_plan* plan, const psgd_linear* op, const void* param, const void* x,
+                                          const void* pre, const void* dy, void* dx, void* grad, int32_t worker,
+                                          int32_t accumulate, void* workspace, void* hip_stream);
+
+/* y = residual + D(x) over [rows][cols] of `dtype`, and dx = D(dy).  residual may be NULL; y may be x or residual, dx may
+ * be dy (the same stride).  rows or cols may be 0.  Errors: PSGD_EINVAL for null or misaligned pointers, negative sizes,
+ * strides below cols, p outside [0, 1]; PSGD_EUNSUPPORTED for sizes or strides of 2^31 and more, or more than 2^42
+ * elements. */
+PSGD_API psgd_status psgd_dropout_forward(psgd_dtype dtype, int64_t rows, int64_t cols, const void* x, int64_t x_stride,
+                                          const void* residual, int64_t residual_stride, void* y, int64_t y_stride,
+                                          double p, const uint64_t* rng, uint64_t offset, void* hip_stream);
+PSGD_API psgd_status psgd_dropout_backward(psgd_dtype dtype, int64_t rows, int64_t cols, const void* dy, int64_t dy_stride,
+                                           void* dx, int64_t dx_stride, double p, const uint64_t* rng, uint64_t offset,
+                                           void* hip_stream);
+
+/* "Random mask" compression (Konecny et al., "Federated learning: strategies for improving communication efficiency",
+ * 2016) in the loop of Random Block and Random K above: of each matrix every worker keeps the same random subset of
+ * the entries of M_w = g_w + e_w, each entry by itself with the same probability; the kept values are averaged over the
+ * workers into Delta', which is zero elsewhere, and e_w <- M_w - Delta'.  The subset follows from rng and offset alone, so
+ * workers with the same words need exchange no positions.  Vector-shaped tensors are averaged uncompressed.  Any
+ * data types; the workspace and the P / Q buffers are not used.
+ *   keep    probability in [0, 1], taken as the multiple of 2^-32 next to it; negative: the plan's budget, kept / (n m)
+ *           of each matrix (psgd_plan_kept) in expectation.  Entry `pos` of the flattened matrix of tensor t: counter
+ *           (pos / 4, t), word pos % 4, kept where that is below 2^32 keep.
+ *   grad    (device, const)  as psgd_step, err (device, in/out) in: e_w ; out: e_w <- M_w - Delta'
+ *   out     (device, out)    [N+L] out_dtype: Delta'
+ * grad, err and out are aligned to four elements.  Errors: PSGD_EINVAL for null or misaligned pointers, keep above 1 or
+ * NaN; PSGD_EUNSUPPORTED for a matrix of more than 2^34 entries. */
+PSGD_API psgd_status psgd_random_mask_step(psgd_plan* plan, const void* grad, float* err, double keep, const uint64_t* rng,
+                                           uint64_t offset, void* out, void* hip_stream);
+
 /* Per-kernel timing for benchmarks.  With profiling enabled, psgd_compress and
  * psgd_decompress record HIP events on the caller's stream around each of their
  * kernels, and psgd_decompress (hence psgd_step) WAITS for the stream at its

@@ -15,6 +15,7 @@ PSGD_OK, PSGD_EINVAL, PSGD_ENOMEM, PSGD_EHIP, PSGD_EUNSUPPORTED = range(5)
 PSGD_F32, PSGD_BF16 = 0, 1
 PSGD_MAX_RANK = 64
 PSGD_N_KERNELS = 8
+ACTIVATIONS = ("identity", "relu", "gelu", "gelu_tanh", "silu")   # in the order of psgd_activation
 
 
 class psgd_shape(C.Structure):
@@ -26,6 +27,13 @@ class psgd_sizes(C.Structure):
         "n_mat_elems", "n_vec_elems", "grad_stride", "err_stride", "out_elems", "p_elems", "q_elems",
         "workspace_bytes", "n_matrices", "n_vectors", "payload_elems", "compressed_elems",
         "bytes_min", "bytes_stream", "kept_elems")]
+
+
+class psgd_linear(C.Structure):
+    _fields_ = ([(n, C.c_int32) for n in ("weight", "bias", "activation", "param_dtype")] +
+                [(n, C.c_int64) for n in ("tokens", "x_stride", "residual_stride", "pre_stride", "y_stride", "dy_stride",
+                                          "dx_stride")] +
+                [("drop", C.c_double), ("rng", C.c_void_p), ("offset", C.c_uint64)])
 
 
 class PsgdError(RuntimeError):
@@ -99,6 +107,18 @@ def load_library(path: Optional[str] = None):
     lib.psgd_plan_check.argtypes = [vp, vp, C.POINTER(i32)]
     lib.psgd_plan_read_trace.restype = C.c_int
     lib.psgd_plan_read_trace.argtypes = [vp, C.POINTER(C.c_uint64), i64, C.POINTER(i64)]
+    lib.psgd_linear_workspace.restype = C.c_int
+    lib.psgd_linear_workspace.argtypes = [vp, C.POINTER(psgd_linear), C.POINTER(i64)]
+    lib.psgd_linear_forward.restype = C.c_int
+    lib.psgd_linear_forward.argtypes = [vp, C.POINTER(psgd_linear), vp, vp, vp, vp, vp, vp, vp]
+    lib.psgd_linear_backward.restype = C.c_int
+    lib.psgd_linear_backward.argtypes = [vp, C.POINTER(psgd_linear), vp, vp, vp, vp, vp, vp, i32, i32, vp, vp]
+    lib.psgd_dropout_forward.restype = C.c_int
+    lib.psgd_dropout_forward.argtypes = [C.c_int, i64, i64, vp, i64, vp, i64, vp, i64, C.c_double, vp, C.c_uint64, vp]
+    lib.psgd_dropout_backward.restype = C.c_int
+    lib.psgd_dropout_backward.argtypes = [C.c_int, i64, i64, vp, i64, vp, i64, C.c_double, vp, C.c_uint64, vp]
+    lib.psgd_random_mask_step.restype = C.c_int
+    lib.psgd_random_mask_step.argtypes = [vp, vp, vp, C.c_double, vp, C.c_uint64, vp, vp]
     lib.psgd_status_string.restype = C.c_char_p
     lib.psgd_status_string.argtypes = [C.c_int]
     lib.psgd_plan_last_error.restype = C.c_char_p
@@ -119,6 +139,22 @@ def _ptr(x) -> Optional[int]:
     if isinstance(x, int):
         return x
     return int(x.data_ptr())
+
+
+def dropout_forward(dtype, rows, cols, x, y, p, rng, residual=None, x_stride=0, residual_stride=0, y_stride=0, offset=0,
+                    stream=None):
+    st = load_library().psgd_dropout_forward(int(dtype), int(rows), int(cols), _ptr(x), int(x_stride), _ptr(residual),
+                                             int(residual_stride), _ptr(y), int(y_stride), float(p), _ptr(rng), int(offset),
+                                             _ptr(stream))
+    if st != PSGD_OK:
+        raise PsgdError(st, "psgd_dropout_forward")
+
+
+def dropout_backward(dtype, rows, cols, dy, dx, p, rng, dy_stride=0, dx_stride=0, offset=0, stream=None):
+    st = load_library().psgd_dropout_backward(int(dtype), int(rows), int(cols), _ptr(dy), int(dy_stride), _ptr(dx),
+                                              int(dx_stride), float(p), _ptr(rng), int(offset), _ptr(stream))
+    if st != PSGD_OK:
+        raise PsgdError(st, "psgd_dropout_backward")
 
 
 class Plan:
@@ -200,6 +236,35 @@ class Plan:
     def random_k_step(self, grad, err, indices, vals, out, stream=None):
         self._check(self._lib.psgd_random_k_step(self._h, _ptr(grad), _ptr(err), _ptr(indices), _ptr(vals), _ptr(out),
                                                  _ptr(stream)), "psgd_random_k_step")
+
+    def random_mask_step(self, grad, err, keep, rng, out, offset=0, stream=None):
+        self._check(self._lib.psgd_random_mask_step(self._h, _ptr(grad), _ptr(err), float(keep), _ptr(rng), int(offset),
+                                                    _ptr(out), _ptr(stream)), "psgd_random_mask_step")
+
+    # -- psgd_linear_*: layers whose weight and bias are tensors of the plan ----
+    def _linear(self, weight, tokens, param_dtype, bias=-1, activation="identity", drop=0.0, rng=None, offset=0, **strides):
+        return psgd_linear(weight=int(weight), bias=int(bias), activation=ACTIVATIONS.index(activation),
+                           param_dtype=int(param_dtype), tokens=int(tokens), drop=float(drop), rng=_ptr(rng),
+                           offset=int(offset), **{k: int(v) for k, v in strides.items()})
+
+    def linear_workspace(self, weight, tokens, param_dtype=PSGD_F32, **op) -> int:
+        n = C.c_int64()
+        op = self._linear(weight, tokens, param_dtype, **op)
+        self._check(self._lib.psgd_linear_workspace(self._h, C.byref(op), C.byref(n)), "psgd_linear_workspace")
+        return n.value
+
+    def linear_forward(self, weight, tokens, param, x, y, workspace, residual=None, pre=None, param_dtype=PSGD_F32, stream=None,
+                       **op):
+        op = self._linear(weight, tokens, param_dtype, **op)
+        self._check(self._lib.psgd_linear_forward(self._h, C.byref(op), _ptr(param), _ptr(x), _ptr(residual), _ptr(pre), _ptr(y),
+                                                  _ptr(workspace), _ptr(stream)), "psgd_linear_forward")
+
+    def linear_backward(self, weight, tokens, param, x, dy, dx, grad, workspace, pre=None, worker=0, accumulate=False,
+                        param_dtype=PSGD_F32, stream=None, **op):
+        op = self._linear(weight, tokens, param_dtype, **op)
+        self._check(self._lib.psgd_linear_backward(self._h, C.byref(op), _ptr(param), _ptr(x), _ptr(pre), _ptr(dy), _ptr(dx),
+                                                   _ptr(grad), int(worker), int(bool(accumulate)), _ptr(workspace),
+                                                   _ptr(stream)), "psgd_linear_backward")
 
     def path(self) -> str:
         """'streaming', 'resident' or 'matrix cores': the kernels psgd_step runs for this plan."""
