@@ -374,7 +374,7 @@ typedef struct {
 PSGD_API psgd_status psgd_linear_workspace(const psgd_plan* plan, const psgd_linear* op, int64_t* bytes);
 
 /* z = x W^T + b ; y = residual + D(act(z)).  x, residual, pre and y have the plan's grad_dtype.
- *   param    (device, const)  flat parameters, laid out like `out` of psgd_decompress
+ *   param    (device, const)  flat parameters, laid out like `out` of psgd_decompress, 16-byte aligned
  *   x        (device, const)  [tokens][k]
  *   residual (device, const)  [tokens][n] or NULL
  *   pre      (device, out)    [tokens][n] or NULL: z, which the backward pass of an activation reads

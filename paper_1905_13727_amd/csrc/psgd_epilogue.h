@@ -1,0 +1,143 @@
+// Activations and the steps behind a product, on the device, in fp32.
+#ifndef PSGD_EPILOGUE_H
+#define PSGD_EPILOGUE_H
+
+#include "psgd_device.h"
+#include "psgd_product.h"
+#include "psgd_random.h"
+
+namespace psgd {
+
+__device__ __forceinline__ float ld_any(const void* p, int64_t at, bool bf) {
+    return bf ? bf16_to_f32(static_cast<const bf16_t*>(p)[at]) : static_cast<const float*>(p)[at];
+}
+__device__ __forceinline__ void st_any(void* p, int64_t at, float v, bool bf) {
+    if (bf) static_cast<bf16_t*>(p)[at] = f32_to_bf16(v);
+    else static_cast<float*>(p)[at] = v;
+}
+
+// 1 / (1 + exp(-v)) and 1 minus that, both without cancellation or overflow
+__device__ __forceinline__ void logistic(float v, float& s, float& rest) {
+    const float e = __expf(-fabsf(v)), big = 1.f / (1.f + e), small = e * big;
+    s = v >= 0.f ? big : small;
+    rest = v >= 0.f ? small : big;
+}
+constexpr float kGeluA = 1.5957691216057308f, kGeluB = 0.044715f;   // 2 sqrt(2 / pi)
+
+__device__ __forceinline__ float act_of(float z, int act) {
+    float s, rest;
+    switch (act) {
+        case PSGD_ACT_RELU: return z < 0.f ? 0.f : z;
+        case PSGD_ACT_GELU: return 0.5f * z * (1.f + erff(z * 0.70710678118654752f));
+        case PSGD_ACT_GELU_TANH: logistic(kGeluA * (z + kGeluB * z * z * z), s, rest); return z * s;   // (1 + tanh u) / 2
+        case PSGD_ACT_SILU: logistic(z, s, rest); return z * s;
+        default: return z;
+    }
+}
+__device__ __forceinline__ float act_slope(float z, int act) {
+    float s, rest;
+    switch (act) {
+        case PSGD_ACT_RELU: return z > 0.f ? 1.f : 0.f;
+        case PSGD_ACT_GELU: return 0.5f * (1.f + erff(z * 0.70710678118654752f)) + z * __expf(-0.5f * z * z) * 0.39894228040143268f;
+        case PSGD_ACT_GELU_TANH:
+            logistic(kGeluA * (z + kGeluB * z * z * z), s, rest);
+            return s + z * s * rest * kGeluA * (1.f + 3.f * kGeluB * z * z);
+        case PSGD_ACT_SILU: logistic(z, s, rest); return s * (1.f + z * rest);
+        default: return 1.f;
+    }
+}
+
+struct Epilogue {
+    float scale;
+    const void* bias;
+    int bias_bf, act;
+    void* pre;
+    int64_t pre_ld;
+    const void* residual;
+    int64_t residual_ld;
+    DropArgs drop;
+};
+
+inline DropArgs drop_of(const DropHost& h) {
+    DropArgs d;
+    d.rng = h.rng;
+    d.offset = h.offset;
+    d.below = h.below;
+    d.factor = h.factor;
+    return d;
+}
+inline Epilogue epilogue_of(const EpilogueHost& h) {
+    return Epilogue{h.scale, h.bias, h.bias_bf, h.act, h.pre, h.pre_ld, h.residual, h.residual_ld, drop_of(h.drop)};
+}
+
+// Eight consecutive elements of a row; `vec`: all exist and lie on a multiple of sixteen bytes
+template <bool BF>
+__device__ __forceinline__ void ld_oct(const void* p, int64_t at, int count, bool vec, float (&x)[8]) {
+    if (vec) {
+        if constexpr (BF) {
+            const v4u t = *reinterpret_cast<const v4u*>(static_cast<const bf16_t*>(p) + at);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) { x[2 * e] = __uint_as_float(t[e] << 16); x[2 * e + 1] = __uint_as_float(t[e] & 0xffff0000u); }
+        } else {
+            const v4f lo = *reinterpret_cast<const v4f*>(static_cast<const float*>(p) + at), hi = *reinterpret_cast<const v4f*>(static_cast<const float*>(p) + at + 4);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) { x[e] = lo[e]; x[4 + e] = hi[e]; }
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = e < count ? ld_any(p, at + e, BF) : 0.f;
+    }
+}
+template <bool BF>
+__device__ __forceinline__ void st_oct(void* p, int64_t at, int count, bool vec, const float (&x)[8]) {
+    if (vec) {
+        if constexpr (BF) {
+            *reinterpret_cast<v4u*>(static_cast<bf16_t*>(p) + at) =
+                v4u{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7])};
+        } else {
+            *reinterpret_cast<v4f*>(static_cast<float*>(p) + at) = v4f{x[0], x[1], x[2], x[3]};
+            *reinterpret_cast<v4f*>(static_cast<float*>(p) + at + 4) = v4f{x[4], x[5], x[6], x[7]};
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (e < count) st_any(p, at + e, x[e], BF);
+    }
+}
+
+// The bias of eight columns from j (a multiple of eight) on; zero where there is none
+__device__ __forceinline__ void bias_oct(const Epilogue& ep, int64_t j, int64_t N, float (&b)[8]) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) b[e] = ep.bias && j + e < N ? ld_any(ep.bias, j + e, ep.bias_bf) : 0.f;
+}
+
+// Columns j .. j + 7 (j a multiple of eight) of row i from their sums: one call of the generator.
+template <bool BF>
+__device__ __forceinline__ void finish_oct(const Epilogue& ep, const Draw& d, void* c, int64_t c_ld, int64_t i, int64_t j, int64_t N,
+                                           const float (&sum)[8], const float (&bias)[8], bool vec) {
+    const int count = N - j < 8 ? (int)(N - j) : 8;
+    vec = vec && count == 8;
+    float v[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = sum[e] * ep.scale + bias[e];
+    if (ep.pre) st_oct<BF>(ep.pre, i * ep.pre_ld + j, count, vec, v);
+    if (ep.act != PSGD_ACT_IDENTITY)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = act_of(v[e], ep.act);
+    if (ep.drop.below) {
+        const Words r = philox(d, (unsigned)(j >> 3), (unsigned)i);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = dropped(r, e, ep.drop.below) ? 0.f : v[e] * ep.drop.factor;
+    }
+    if (ep.residual) {
+        float x[8];
+        ld_oct<BF>(ep.residual, i * ep.residual_ld + j, count, vec, x);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] += x[e];
+    }
+    st_oct<BF>(c, i * c_ld + j, count, vec, v);
+}
+
+}  // namespace psgd
+
+#endif

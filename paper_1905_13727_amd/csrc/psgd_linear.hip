@@ -1,158 +1,99 @@
-// The linear layer of a plan: y = residual + D(act(x W^T + b)) and its backward pass.
+// The linear layer of a plan: y = residual + D(act(x W^T + b)) and its backward pass.  Here what surrounds the products:
+// operands laid out for them where they are not yet, dz and the bias gradient, and which launches a call is.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
 #include <string>
 
-#include "psgd_device.h"
-#include "psgd_operators.h"
-#include "psgd_random.h"
+#include "psgd_epilogue.h"
 
 namespace psgd {
 
-__device__ __forceinline__ float ld_any(const void* p, int64_t at, bool bf) {
-    return bf ? bf16_to_f32(static_cast<const bf16_t*>(p)[at]) : static_cast<const float*>(p)[at];
-}
-__device__ __forceinline__ void st_any(void* p, int64_t at, float v, bool bf) {
-    if (bf) static_cast<bf16_t*>(p)[at] = f32_to_bf16(v);
-    else static_cast<float*>(p)[at] = v;
-}
-
-// ---- activations, in fp32 -------------------------------------------------------------------------------------------
-
-// 1 / (1 + exp(-v)) and 1 minus that, both without cancellation or overflow
-__device__ __forceinline__ void logistic(float v, float& s, float& rest) {
-    const float e = __expf(-fabsf(v)), big = 1.f / (1.f + e), small = e * big;
-    s = v >= 0.f ? big : small;
-    rest = v >= 0.f ? small : big;
-}
-constexpr float kGeluA = 1.5957691216057308f, kGeluB = 0.044715f;   // 2 sqrt(2 / pi)
-
-__device__ __forceinline__ float act_of(float z, int act) {
-    float s, rest;
-    switch (act) {
-        case PSGD_ACT_RELU: return z < 0.f ? 0.f : z;
-        case PSGD_ACT_GELU: return 0.5f * z * (1.f + erff(z * 0.70710678118654752f));
-        case PSGD_ACT_GELU_TANH: logistic(kGeluA * (z + kGeluB * z * z * z), s, rest); return z * s;   // (1 + tanh u) / 2
-        case PSGD_ACT_SILU: logistic(z, s, rest); return z * s;
-        default: return z;
-    }
-}
-__device__ __forceinline__ float act_slope(float z, int act) {
-    float s, rest;
-    switch (act) {
-        case PSGD_ACT_RELU: return z > 0.f ? 1.f : 0.f;
-        case PSGD_ACT_GELU: return 0.5f * (1.f + erff(z * 0.70710678118654752f)) + z * __expf(-0.5f * z * z) * 0.39894228040143268f;
-        case PSGD_ACT_GELU_TANH:
-            logistic(kGeluA * (z + kGeluB * z * z * z), s, rest);
-            return s + z * s * rest * kGeluA * (1.f + 3.f * kGeluB * z * z);
-        case PSGD_ACT_SILU: logistic(z, s, rest); return s * (1.f + z * rest);
-        default: return 1.f;
-    }
-}
-
-// ---- product --------------------------------------------------------------------------------------------------------
-
-struct Epilogue {
-    const void* bias;
-    bool bias_bf;
-    int act;
-    void* pre;
-    int64_t pre_ld;
-    const void* residual;
-    int64_t residual_ld;
-    DropArgs drop;
-    bool accumulate;
-    float scale;
-};
-
-// C[i][j] = sum_l A(i, l) B(j, l), element (i, l) of A at i * a_i + l * a_l, and the epilogue
-__global__ __launch_bounds__(kBlock) void k_product(const void* A, int64_t a_i, int64_t a_l, bool a_bf, const void* B, int64_t b_j,
-                                                    int64_t b_l, bool b_bf, bool round_b, void* C, int64_t c_ld, bool c_bf, int64_t M,
-                                                    int64_t N, int64_t K, Epilogue ep) {
-    __shared__ float As[16][65], Bs[16][65];
-    const int64_t i0 = (int64_t)blockIdx.x * 64, j0 = (int64_t)blockIdx.y * 64;
-    const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-    float acc[4][4] = {};
-    for (int64_t l0 = 0; l0 < K; l0 += 16) {
-        for (int e = threadIdx.x; e < 1024; e += kBlock) {
-            const int r = e >> 4, l = e & 15;
-            const bool in = l0 + l < K;
-            As[l][r] = in && i0 + r < M ? ld_any(A, (i0 + r) * a_i + (l0 + l) * a_l, a_bf) : 0.f;
-            float b = in && j0 + r < N ? ld_any(B, (j0 + r) * b_j + (l0 + l) * b_l, b_bf) : 0.f;
-            Bs[l][r] = round_b ? bf16_to_f32(f32_to_bf16(b)) : b;
-        }
-        __syncthreads();
-        for (int l = 0; l < 16; ++l)
-            for (int a = 0; a < 4; ++a)
-                for (int b = 0; b < 4; ++b) acc[a][b] += As[l][ty + 16 * a] * Bs[l][tx * 4 + b];
-        __syncthreads();
-    }
-    Draw d{};
-    if (ep.drop.below) d = make_draw(ep.drop.rng, ep.drop.offset);
-    for (int a = 0; a < 4; ++a) {
-        const int64_t i = i0 + ty + 16 * a;
-        if (i >= M) continue;
-        for (int b = 0; b < 4; ++b) {
-            const int64_t j = j0 + tx * 4 + b;
-            if (j >= N) continue;
-            float z = acc[a][b] * ep.scale;
-            if (ep.bias) z += ld_any(ep.bias, j, ep.bias_bf);
-            if (ep.pre) st_any(ep.pre, i * ep.pre_ld + j, z, c_bf);
-            float v = act_of(z, ep.act);
-            if (ep.drop.below) v = dropped(philox(d, (unsigned)(j >> 3), (unsigned)i), (int)(j & 7), ep.drop.below) ? 0.f : v * ep.drop.factor;
-            if (ep.residual) v += ld_any(ep.residual, i * ep.residual_ld + j, c_bf);
-            if (ep.accumulate) v += ld_any(C, i * c_ld + j, c_bf);
-            st_any(C, i * c_ld + j, v, c_bf);
-        }
-    }
+// dst [rows][dst_ld] = src [rows][cols], rounded if dst is bf16 and src is not; columns up to dst_ld are zero.
+// One lane: eight columns.
+template <bool SBF, bool DBF>
+__global__ __launch_bounds__(kBlock) void k_lay_out(const void* src, int64_t src_ld, void* dst, int64_t dst_ld, int64_t rows, int64_t cols,
+                                                    int vec) {
+    const int64_t per_row = (dst_ld + 7) / 8, at = (int64_t)blockIdx.x * kBlock + threadIdx.x;
+    if (at >= rows * per_row) return;
+    const int64_t row = at / per_row, j = 8 * (at - row * per_row);
+    float x[8];
+    const int count = cols - j < 8 ? (int)(cols - j) : 8;
+    ld_oct<SBF>(src, row * src_ld + j, count, vec && count == 8, x);
+    const int to = dst_ld - j < 8 ? (int)(dst_ld - j) : 8;
+    st_oct<DBF>(dst, row * dst_ld + j, to, to == 8, x);
 }
 
 // dz = D(dy) act'(pre) without the factor of the elements that stay, which goes into the products' epilogues: where the
 // slope is 0 or 1 dz is then exact in any type.  And the sum of every column over a block of rows.
 // One lane: eight columns (one call of the generator) and every eighth row of the block.
-constexpr int kDzRows = 128;
+constexpr int kDzRows = 64;
 
-__global__ __launch_bounds__(kBlock) void k_dz(const void* dy, int64_t dy_ld, const void* pre, int64_t pre_ld, int act, bool bf,
-                                               DropArgs drop, void* dz, int64_t dz_ld, float* partial, int64_t T, int64_t n) {
-    __shared__ float sums[8][257];
-    const int64_t c0 = (int64_t)blockIdx.x * 256 + 8 * (threadIdx.x & 31);
-    const int64_t t0 = (int64_t)blockIdx.y * kDzRows, t1 = t0 + kDzRows < T ? t0 + kDzRows : T;
+template <bool BF>
+__global__ __launch_bounds__(kBlock) void k_dz(const void* dy, int64_t dy_ld, const void* pre, int64_t pre_ld, int act, DropArgs drop,
+                                               void* dz, int64_t dz_ld, float* partial, int64_t T, int64_t n, int vec) {
+    __shared__ float sums[8][264];
+    const int lane_c = threadIdx.x & 31, lane_t = threadIdx.x >> 5;
+    const int64_t blocks_c = (n + 255) / 256, bt = blockIdx.x / blocks_c, bc = blockIdx.x - bt * blocks_c;
+    const int64_t c0 = bc * 256 + 8 * lane_c;
+    const int64_t t0 = bt * kDzRows, t1 = t0 + kDzRows < T ? t0 + kDzRows : T;
+    const int count = n - c0 < 8 ? (int)(n - c0) : 8;
+    const bool whole = vec && count == 8;
     Draw d{};
     if (drop.below) d = make_draw(drop.rng, drop.offset);
     float s[8] = {};
-    for (int64_t t = t0 + (threadIdx.x >> 5); t < t1; t += 8) {
-        Words r{};
-        if (drop.below) r = philox(d, (unsigned)(c0 >> 3), (unsigned)t);
-        for (int j = 0; j < 8 && c0 + j < n; ++j) {
-            float v = 0.f;
-            if (!dropped(r, j, drop.below)) {
-                v = ld_any(dy, t * dy_ld + c0 + j, bf);
-                if (act != PSGD_ACT_IDENTITY) v *= act_slope(ld_any(pre, t * pre_ld + c0 + j, bf), act);
+    if (count > 0) {
+        for (int64_t t = t0 + lane_t; t < t1; t += 8) {
+            float v[8];
+            ld_oct<BF>(dy, t * dy_ld + c0, count, whole, v);
+            if (act != PSGD_ACT_IDENTITY) {
+                float z[8];
+                ld_oct<BF>(pre, t * pre_ld + c0, count, whole, z);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] *= act_slope(z[j], act);
             }
-            if (dz) st_any(dz, t * dz_ld + c0 + j, v, bf);
-            s[j] += v;
+            if (drop.below) {
+                const Words r = philox(d, (unsigned)(c0 >> 3), (unsigned)t);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] = dropped(r, j, drop.below) ? 0.f : v[j];
+            }
+            if (dz) {   // up to the end of its rows: zero behind the last column
+                if (count < 8)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) v[j] = j < count ? v[j] : 0.f;
+                const int to = dz_ld - c0 < 8 ? (int)(dz_ld - c0) : 8;
+                st_oct<BF>(dz, t * dz_ld + c0, to, to == 8, v);
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) s[j] += v[j];
         }
     }
     if (!partial) return;
-    for (int j = 0; j < 8; ++j) sums[threadIdx.x >> 5][8 * (threadIdx.x & 31) + j] = s[j];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) sums[lane_t][8 * lane_c + j] = s[j];
     __syncthreads();
-    const int64_t col = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int64_t col = bc * 256 + threadIdx.x;
     if (col >= n) return;
     float v = 0.f;
     for (int i = 0; i < 8; ++i) v += sums[i][threadIdx.x];
-    partial[(int64_t)blockIdx.y * n + col] = v;
+    partial[bt * n + col] = v;
 }
 
-__global__ __launch_bounds__(kBlock) void k_column_sum(const float* partial, int64_t count, int64_t n, float scale, void* db, bool bf,
-                                                       bool accumulate) {
-    const int64_t col = (int64_t)blockIdx.x * kBlock + threadIdx.x;
-    if (col >= n) return;
+// db from the blocks' sums: a workgroup 64 columns, its four waves every fourth block, joined in order
+template <bool BF>
+__global__ __launch_bounds__(kBlock) void k_column_sum(const float* partial, int64_t count, int64_t n, float scale, void* db, int accumulate) {
+    __shared__ float sums[4][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t col = (int64_t)blockIdx.x * 64 + lane;
     float v = 0.f;
-    for (int64_t i = 0; i < count; ++i) v += partial[i * n + col];
-    v *= scale;
-    if (accumulate) v += ld_any(db, col, bf);
-    st_any(db, col, v, bf);
+    if (col < n)
+        for (int64_t i = wave; i < count; i += 4) v += partial[i * n + col];
+    sums[wave][lane] = v;
+    __syncthreads();
+    if (wave || col >= n) return;
+    v = ((sums[0][lane] + sums[1][lane]) + (sums[2][lane] + sums[3][lane])) * scale;
+    if (accumulate) v += ld_any(db, col, BF);
+    st_any(db, col, v, BF);
 }
 
 namespace {
@@ -166,81 +107,151 @@ bool failed(const char* name, std::string* what) {
     return true;
 }
 
-DropArgs drop_of(const DropHost& h) {
-    DropArgs d;
-    d.rng = h.rng;
-    d.offset = h.offset;
-    d.below = h.below;
-    d.factor = h.factor;
-    return d;
+bool vec_aligned(const void* p, int64_t ld, int64_t z) { return !p || (reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld * z % 16 == 0); }
+
+// Where the parts of the workspace are
+struct Parts {
+    int64_t w, x, dz, db, partial, bytes;   // offsets; w = -1: the weights are read where they are
+    int64_t k_ld, n_ld;                     // row lengths of laid-out operands
+};
+
+Parts parts_of(const LinearCall& c) {
+    Parts p{};
+    const int64_t z = c.bf16 ? 2 : 4, run = 16 / z;
+    if (c.T == 0) return p;
+    p.k_ld = up(c.k, run);
+    p.n_ld = up(c.n, run);
+    int64_t at = 0;
+    auto take = [&](int64_t bytes) { const int64_t was = at; at += up(bytes, 256); return was; };
+    p.w = c.param_bf16 != c.bf16 || c.k % run ? take(c.n * p.k_ld * z) : -1;
+    p.x = take(c.T * p.k_ld * z);
+    p.dz = take(c.T * p.n_ld * z);
+    p.db = take(up(c.T, kDzRows) / kDzRows * c.n * 4);
+    p.partial = take(std::max({product_partial_bytes(c.bf16, c.T, c.n, c.k), product_partial_bytes(c.bf16, c.T, c.k, c.n),
+                               product_partial_bytes(c.bf16, c.n, c.k, c.T)}));
+    p.bytes = at;
+    return p;
+}
+
+bool lay_out(const void* src, int64_t src_ld, bool src_bf, void* dst, int64_t dst_ld, bool dst_bf, int64_t rows, int64_t cols, hipStream_t s,
+             std::string* what) {
+    const int64_t blocks = (rows * ((dst_ld + 7) / 8) + kBlock - 1) / kBlock;
+    const int vec = vec_aligned(src, src_ld, src_bf ? 2 : 4);
+    auto k = src_bf ? k_lay_out<true, true> : dst_bf ? k_lay_out<false, true> : k_lay_out<false, false>;
+    hipLaunchKernelGGL(k, dim3((unsigned)blocks), dim3(kBlock), 0, s, src, src_ld, dst, dst_ld, rows, cols, vec);
+    return !failed("k_lay_out", what);
+}
+
+// The weights or the input as an operand of a product: in place if rows and base allow, else laid out
+bool weights(const LinearCall& c, const Parts& p, const void** w, int64_t* ld, std::string* what) {
+    *w = c.w;
+    *ld = c.k;
+    if (p.w < 0) return true;
+    *w = static_cast<char*>(c.workspace) + p.w;
+    *ld = p.k_ld;
+    return lay_out(c.w, c.k, c.param_bf16, const_cast<void*>(*w), *ld, c.bf16, c.n, c.k, static_cast<hipStream_t>(c.stream), what);
+}
+bool input(const LinearCall& c, const Parts& p, const void** x, int64_t* ld, std::string* what) {
+    *x = c.x;
+    *ld = c.x_ld;
+    const int64_t z = c.bf16 ? 2 : 4;
+    if (vec_aligned(c.x, c.x_ld, z) && c.k * z % 16 == 0) return true;
+    *x = static_cast<char*>(c.workspace) + p.x;
+    *ld = p.k_ld;
+    return lay_out(c.x, c.x_ld, c.bf16, const_cast<void*>(*x), *ld, c.bf16, c.T, c.k, static_cast<hipStream_t>(c.stream), what);
 }
 
 }  // namespace
 
-int64_t linear_workspace_bytes(const LinearCall& c) {
-    const int64_t z = c.bf16 ? 2 : 4;
-    return up(c.T * c.n * z, 256) + up((c.T + kDzRows - 1) / kDzRows * c.n * 4, 256);
-}
+int64_t linear_workspace_bytes(const LinearCall& c) { return parts_of(c).bytes; }
 
 psgd_status launch_linear_forward(const LinearCall& c, std::string* what) {
-    Epilogue ep{};
-    ep.bias = c.bias;
-    ep.bias_bf = c.param_bf16;
-    ep.act = c.act;
-    ep.pre = c.pre;
-    ep.pre_ld = c.pre_ld;
-    ep.residual = c.residual;
-    ep.residual_ld = c.residual_ld;
-    ep.drop = drop_of(c.drop);
-    ep.scale = 1.f;
-    const dim3 grid((unsigned)((c.T + 63) / 64), (unsigned)((c.n + 63) / 64));
-    hipLaunchKernelGGL(k_product, grid, dim3(kBlock), 0, static_cast<hipStream_t>(c.stream), c.x, c.x_ld, (int64_t)1, c.bf16, c.w, c.k,
-                       (int64_t)1, c.param_bf16, c.bf16, c.y, c.y_ld, c.bf16, c.T, c.n, c.k, ep);
-    return failed("k_product", what) ? PSGD_EHIP : PSGD_OK;
+    const Parts p = parts_of(c);
+    ProductCall q{};
+    q.bf16 = c.bf16;
+    q.a_along = q.b_along = true;
+    if (!weights(c, p, &q.b, &q.b_ld, what) || !input(c, p, &q.a, &q.a_ld, what)) return PSGD_EHIP;
+    q.c = c.y;
+    q.c_ld = c.y_ld;
+    q.M = c.T;
+    q.N = c.n;
+    q.K = c.k;
+    q.ep.bias = c.bias;
+    q.ep.bias_bf = c.param_bf16;
+    q.ep.act = c.act;
+    q.ep.pre = c.pre;
+    q.ep.pre_ld = c.pre_ld;
+    q.ep.residual = c.residual;
+    q.ep.residual_ld = c.residual_ld;
+    q.ep.drop = c.drop;
+    q.partial = reinterpret_cast<float*>(static_cast<char*>(c.workspace) + p.partial);
+    q.stream = static_cast<hipStream_t>(c.stream);
+    return launch_product(q, what);
 }
 
 psgd_status launch_linear_backward(const LinearCall& c, std::string* what) {
     const hipStream_t s = static_cast<hipStream_t>(c.stream);
+    const Parts p = parts_of(c);
     const int64_t z = c.bf16 ? 2 : 4;
-    Epilogue ep{};
-    ep.scale = c.drop.below ? c.drop.factor : 1.f;
+    const float scale = c.drop.below ? c.drop.factor : 1.f;
+    if (c.T == 0 && c.accumulate) return PSGD_OK;
+    char* const ws = static_cast<char*>(c.workspace);
+    const int64_t blocks = up(c.T, kDzRows) / kDzRows;
+    const void* dz = c.dy;
+    int64_t dz_ld = c.dy_ld;
     if (c.T > 0) {
-        char* ws = static_cast<char*>(c.workspace);
-        void* dz = ws;
-        float* partial = reinterpret_cast<float*>(ws + up(c.T * c.n * z, 256));
-        const int64_t blocks = (c.T + kDzRows - 1) / kDzRows;
-        hipLaunchKernelGGL(k_dz, dim3((unsigned)((c.n + 255) / 256), (unsigned)blocks), dim3(kBlock), 0, s, c.dy, c.dy_ld, c.pre, c.pre_ld, c.act,
-                           c.bf16, drop_of(c.drop), dz, c.n, partial, c.T, c.n);
-        if (failed("k_dz", what)) return PSGD_EHIP;
-        if (c.dx) {
-            hipLaunchKernelGGL(k_product, dim3((unsigned)((c.T + 63) / 64), (unsigned)((c.k + 63) / 64)), dim3(kBlock), 0, s, dz, c.n, (int64_t)1,
-                               c.bf16, c.w, (int64_t)1, c.k, c.param_bf16, c.bf16, c.dx, c.dx_ld, c.bf16, c.T, c.k, c.n, ep);
-            if (failed("k_product", what)) return PSGD_EHIP;
+        const bool direct = c.act == PSGD_ACT_IDENTITY && !c.drop.below && vec_aligned(c.dy, c.dy_ld, z) && c.n * z % 16 == 0;
+        if (!direct) {
+            dz = ws + p.dz;
+            dz_ld = p.n_ld;
         }
-        if (c.db) {
-            hipLaunchKernelGGL(k_column_sum, dim3((unsigned)((c.n + kBlock - 1) / kBlock)), dim3(kBlock), 0, s, partial, blocks, c.n, ep.scale, c.db,
-                               c.bf16, c.accumulate);
-            if (failed("k_column_sum", what)) return PSGD_EHIP;
+        if (!direct || c.db) {
+            auto k = c.bf16 ? k_dz<true> : k_dz<false>;
+            const int vec = vec_aligned(c.dy, c.dy_ld, z) && (c.act == PSGD_ACT_IDENTITY || vec_aligned(c.pre, c.pre_ld, z));
+            if ((c.n + 255) / 256 * blocks > 0x7fffffffLL) return PSGD_EUNSUPPORTED;
+            hipLaunchKernelGGL(k, dim3((unsigned)((c.n + 255) / 256 * blocks)), dim3(kBlock), 0, s, c.dy, c.dy_ld, c.pre, c.pre_ld, c.act, drop_of(c.drop),
+                               direct ? nullptr : const_cast<void*>(dz), dz_ld, c.db ? reinterpret_cast<float*>(ws + p.db) : nullptr, c.T, c.n, vec);
+            if (failed("k_dz", what)) return PSGD_EHIP;
         }
-        ep.accumulate = c.accumulate;
-        if (c.dw) {
-            hipLaunchKernelGGL(k_product, dim3((unsigned)((c.n + 63) / 64), (unsigned)((c.k + 63) / 64)), dim3(kBlock), 0, s, dz, (int64_t)1, c.n,
-                               c.bf16, c.x, (int64_t)1, c.x_ld, c.bf16, false, c.dw, c.k, c.bf16, c.n, c.k, c.T, ep);
-            if (failed("k_product", what)) return PSGD_EHIP;
-        }
-        return PSGD_OK;
-    }
-    if (c.accumulate) return PSGD_OK;
-    // no tokens: gradients of zero
-    if (c.dw) {
-        hipLaunchKernelGGL(k_product, dim3((unsigned)((c.n + 63) / 64), (unsigned)((c.k + 63) / 64)), dim3(kBlock), 0, s, nullptr, (int64_t)1, c.n,
-                           c.bf16, nullptr, (int64_t)1, c.k, c.bf16, false, c.dw, c.k, c.bf16, c.n, c.k, (int64_t)0, ep);
-        if (failed("k_product", what)) return PSGD_EHIP;
     }
     if (c.db) {
-        hipLaunchKernelGGL(k_column_sum, dim3((unsigned)((c.n + kBlock - 1) / kBlock)), dim3(kBlock), 0, s, nullptr, (int64_t)0, c.n, 1.f, c.db,
-                           c.bf16, false);
+        auto k = c.bf16 ? k_column_sum<true> : k_column_sum<false>;
+        hipLaunchKernelGGL(k, dim3((unsigned)((c.n + 63) / 64)), dim3(kBlock), 0, s, reinterpret_cast<const float*>(ws + p.db), blocks, c.n, scale,
+                           c.db, (int)c.accumulate);
         if (failed("k_column_sum", what)) return PSGD_EHIP;
+    }
+    ProductCall q{};
+    q.bf16 = c.bf16;
+    q.ep.scale = scale;
+    q.partial = reinterpret_cast<float*>(ws + p.partial);
+    q.stream = s;
+    q.a = dz;
+    q.a_ld = dz_ld;
+    q.N = c.k;
+    if (c.dx && c.T > 0) {
+        q.a_along = true;
+        if (!weights(c, p, &q.b, &q.b_ld, what)) return PSGD_EHIP;
+        q.c = c.dx;
+        q.c_ld = c.dx_ld;
+        q.M = c.T;
+        q.K = c.n;
+        const psgd_status st = launch_product(q, what);
+        if (st != PSGD_OK) return st;
+    }
+    if (c.dw) {
+        q.a_along = false;
+        q.b = nullptr;
+        q.b_ld = 0;
+        if (c.T > 0 && !input(c, p, &q.b, &q.b_ld, what)) return PSGD_EHIP;
+        q.c = c.dw;
+        q.c_ld = c.k;
+        q.M = c.n;
+        q.K = c.T;
+        if (c.accumulate) {
+            q.ep.residual = c.dw;
+            q.ep.residual_ld = c.k;
+        }
+        return launch_product(q, what);
     }
     return PSGD_OK;
 }

@@ -84,7 +84,7 @@ psgd_status psgd_linear_forward(psgd_plan* plan, const psgd_linear* op, const vo
     if (!param) return PSGD_EINVAL;
     if (c.T == 0) return PSGD_OK;
     const size_t z = c.bf16 ? 2 : 4;
-    if (!x || !y || !aligned(x, z) || !aligned(y, z) || !aligned(residual, z) || !aligned(pre, z) || !aligned(param, c.param_bf16 ? 2 : 4))
+    if (!x || !y || !aligned(x, z) || !aligned(y, z) || !aligned(residual, z) || !aligned(pre, z) || !aligned(param, 16))
         return PSGD_EINVAL;
     if (psgd::linear_workspace_bytes(c) > 0 && (!workspace || !aligned(workspace, 256))) return PSGD_EINVAL;
     c.w = at(param, plan->tensor_flat_off[op->weight], c.param_bf16);
@@ -115,7 +115,7 @@ psgd_status psgd_linear_backward(psgd_plan* plan, const psgd_linear* op, const v
     if (c.T > 0) {
         if (!dy || !aligned(dy, z)) return PSGD_EINVAL;
         if (c.act != PSGD_ACT_IDENTITY && (!pre || !aligned(pre, z))) return PSGD_EINVAL;
-        if (dx && (!param || !aligned(param, c.param_bf16 ? 2 : 4))) return PSGD_EINVAL;
+        if (dx && (!param || !aligned(param, 16))) return PSGD_EINVAL;
         if (grad && (!x || !aligned(x, z))) return PSGD_EINVAL;
         if (psgd::linear_workspace_bytes(c) > 0 && (!workspace || !aligned(workspace, 256))) return PSGD_EINVAL;
     }

@@ -1,0 +1,52 @@
+// Products of the linear layer on the matrix cores: C[i][j] = sum_l A(i, l) B(j, l) with an epilogue.
+#ifndef PSGD_PRODUCT_H
+#define PSGD_PRODUCT_H
+
+#include <stdint.h>
+
+#include <string>
+
+#include "psgd_operators.h"
+
+namespace psgd {
+
+// What follows the sums, in this order: times scale, plus bias, stored as `pre`, activation, dropout, plus residual (or plus what C
+// holds: residual = C), stored.
+struct EpilogueHost {
+    float scale = 1.f;
+    const void* bias = nullptr;
+    bool bias_bf = false;
+    int act = PSGD_ACT_IDENTITY;
+    void* pre = nullptr;
+    int64_t pre_ld = 0;
+    const void* residual = nullptr;
+    int64_t residual_ld = 0;
+    DropHost drop{};
+};
+
+// Either operand lies along the contraction (`along`: element (i, l) at i * ld + l) or across it (l * ld + i).  Bases are aligned
+// to 16 bytes, ld is a multiple of 16 bytes, and so is the contiguous extent, or what follows it up to the next multiple is
+// readable and zero.
+struct ProductCall {
+    bool bf16;
+    const void* a;
+    int64_t a_ld;
+    bool a_along;
+    const void* b;
+    int64_t b_ld;
+    bool b_along;
+    void* c;
+    int64_t c_ld;
+    int64_t M, N, K;
+    EpilogueHost ep;
+    float* partial;          // scratch of product_partial_bytes
+    hipStream_t stream;
+};
+
+// Scratch for the product and for any with fewer rows M
+int64_t product_partial_bytes(bool bf16, int64_t M, int64_t N, int64_t K);
+psgd_status launch_product(const ProductCall& c, std::string* what);
+
+}  // namespace psgd
+
+#endif

@@ -1,0 +1,367 @@
+// Products of the linear layer on the matrix cores: C[i][j] = sum_l A(i, l) B(j, l).  x W^T has both operands along the
+// contraction, dz W the second across it, dz^T x both.
+//
+// A workgroup owns a tile of BM x BN outputs and goes along the contraction in steps of 128 bytes a row (64 bf16, 32 fp32), two
+// steps in LDS at a time: while the waves read one, the next is loaded straight into LDS, sixteen bytes a lane.
+// Such a load writes 64 consecutive chunks of sixteen bytes, so which chunk of the operand lies where is decided by
+// which one a lane asks for; the places are permuted so that the reads of a wave meet no bank twice:
+//   along    row r holds its eight chunks in the order c ^ key(r), key the three bits in which the eight rows that are
+//            read together differ;
+//   across   row l of the contraction holds its chunks in the order c ^ f(l), f such that the four rows of a transposing read
+//            (ds_read_b64_tr_b16: four rows of the contraction, sixteen of the output) lie in different banks.
+// The sums go through LDS once more, 64 rows a wave at a time: a lane then holds eight consecutive columns of a row, one
+// store of sixteen bytes (bf16) and one call of the generator.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+
+#include "psgd_epilogue.h"
+
+namespace psgd {
+
+typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
+typedef short v4s __attribute__((ext_vector_type(4)));
+typedef short v8s __attribute__((ext_vector_type(8)));
+typedef __attribute__((address_space(3))) char lds_char;
+
+constexpr int kLanded = 0x0f70;   // vmcnt(0): loads to LDS count there; the other counters are left alone
+
+// ---- one operand of a tile ------------------------------------------------------------------------------------------
+
+// ROWS: outputs of the tile in this operand's dimension; Z: bytes an element; THREADS of the workgroup
+template <int ROWS, int Z, bool ALONG, int THREADS>
+struct Operand {
+    static constexpr int kElems = 16 / Z;                 // a chunk
+    static constexpr int kStep = 128 / Z;                 // contraction of a step
+    static constexpr int kRowChunks = ALONG ? 8 : ROWS / kElems;
+    static constexpr int kBytes = ROWS * 128;
+    static constexpr int kLoads = kBytes / 16 / THREADS;
+    static_assert(kBytes % (16 * THREADS) == 0, "whole loads");
+
+    static __device__ __forceinline__ int key(int line) {
+        if constexpr (ALONG) return line & 7;
+        else if constexpr (Z == 2) return ((line & 3) << 1) | (line & 8);
+        else return 0;
+    }
+    // byte offsets of this lane's chunks from the operand's base for the first step.  Outputs past the end are clamped to the last
+    // ones: what they give is not stored.
+    static __device__ __forceinline__ void sources(unsigned (&off)[kLoads], int64_t ld, int64_t extent) {
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int q = i * THREADS + threadIdx.x, line = q / kRowChunks, c = (q % kRowChunks) ^ key(line);
+            if constexpr (ALONG) {
+                const int row = line < extent ? line : (int)extent - 1;
+                off[i] = (unsigned)(row * ld * Z + c * 16);
+            } else {
+                const int last = ((int)(extent < ROWS ? extent : ROWS) + kElems - 1) / kElems - 1;
+                off[i] = (unsigned)(line * ld * Z + (c < last ? c : last) * 16);
+            }
+        }
+    }
+    // whether chunk i of a step with `left` elements of the contraction to go exists
+    static __device__ __forceinline__ bool inside(int i, int left) {
+        const int q = i * THREADS + threadIdx.x, line = q / kRowChunks;
+        if constexpr (ALONG) return ((q % kRowChunks) ^ key(line)) * kElems < left;
+        else return line < left;
+    }
+    static __device__ __forceinline__ void load(const char* base, const unsigned (&off)[kLoads], lds_char* to) {
+        const buf_rsrc r = make_rsrc(base, 0x7fffffff);
+        lds_char* at = to + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave) * (kWave * 16);
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)(at + i * THREADS * 16), 16, (int)off[i], 0, 0, 0);
+    }
+    // the last step, cut short: chunks past the end of the contraction are zero
+    static __device__ __forceinline__ void load_cut(const char* base, const unsigned (&off)[kLoads], lds_char* to, int left) {
+        const buf_rsrc r = make_rsrc(base, 0x7fffffff);
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            v4u t = v4u{0, 0, 0, 0};
+            if (inside(i, left)) t = __builtin_amdgcn_raw_buffer_load_b128(r, (int)off[i], 0, 0);
+            *reinterpret_cast<__attribute__((address_space(3))) v4u*>(to + (i * THREADS + threadIdx.x) * 16) = t;
+        }
+    }
+    static __device__ __forceinline__ int64_t step_bytes(int64_t ld) { return ALONG ? 128 : kStep * ld * Z; }
+
+    // ---- fragments of half `h` (0, 1) of a step: lane i of lane group g reads output 16 f + i.  bf16: its eight of 32
+    static __device__ __forceinline__ v8bf frag16(const lds_char* s, int first, int f, int h) {
+        const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
+        if constexpr (ALONG) {
+            const int row = first + 16 * f + i;
+            const int c = (4 * h + g) ^ key(row);
+            return *reinterpret_cast<const __attribute__((address_space(3))) v8bf*>(s + row * 128 + c * 16);
+        } else {
+            // the four lines l .. l + 3 of a lane group's eight, sixteen outputs each: lane i asks for line i / 4, outputs 4 (i % 4)
+            const int l = 32 * h + 8 * g + (i >> 2), m = first + 16 * f + 4 * (i & 3);
+            const lds_char* p = s + l * (ROWS * Z) + ((((m * Z) >> 4) ^ key(l)) << 4) + ((m * Z) & 15);
+            typedef __attribute__((address_space(3))) v4s* lds_v4s;
+            const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s)p);
+            const v4s hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s)(p + 4 * (ROWS * Z)));   // key(l + 4) = key(l)
+            const v8s both = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+            return __builtin_bit_cast(v8bf, both);
+        }
+    }
+    // sixteen of the contraction, four to a lane: element e of lane group g is number 16 h + 4 g + e
+    static __device__ __forceinline__ v4f frag32(const lds_char* s, int first, int f, int h) {
+        const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
+        if constexpr (ALONG) {
+            const int row = first + 16 * f + i;
+            return *reinterpret_cast<const __attribute__((address_space(3))) v4f*>(s + row * 128 + (((4 * h + g) ^ key(row)) << 4));
+        } else {
+            v4f t;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                t[e] = *reinterpret_cast<const __attribute__((address_space(3))) float*>(s + (16 * h + 4 * g + e) * (ROWS * Z) + (first + 16 * f + i) * 4);
+            return t;
+        }
+    }
+};
+
+// ---- tiles ----------------------------------------------------------------------------------------------------------
+
+// The workgroups that run at the same time on one die (own L2) get neighbouring tiles: numbers are dealt to the eight dies in
+// ranges, and a range goes along the rows of C in bands of eight tiles.
+__device__ __forceinline__ void tile_of(int64_t number, int64_t count, int64_t tiles_m, int64_t tiles_n, int64_t& tm, int64_t& tn) {
+    const int64_t each = count / 8, more = count % 8, die = number % 8;
+    int64_t t = die * each + (die < more ? die : more) + number / 8;
+    constexpr int64_t kBand = 8;
+    const int64_t band = t / (kBand * tiles_n), first = band * kBand, high = tiles_m - first < kBand ? tiles_m - first : kBand;
+    t -= band * kBand * tiles_n;
+    tm = first + t % high;
+    tn = t / high;
+}
+
+template <bool BF, bool AA, bool BA, int WM, int WN, int MF>
+struct Shape {   // WM x WN waves, each MF x 4 fragments of 16 x 16
+    static constexpr int BM = WM * MF * 16, BN = WN * 64, T = WM * WN * kWave;
+    static constexpr int Z = BF ? 2 : 4;
+    typedef Operand<BM, Z, AA, T> A;
+    typedef Operand<BN, Z, BA, T> B;
+    static constexpr int kLds = 2 * (A::kBytes + B::kBytes);
+    static_assert(kLds >= WM * WN * 64 * 64 * 4 && MF % 4 == 0, "64 rows of sums a wave");
+};
+
+// grid: tiles_m * tiles_n * splits.  With several splits of the contraction the sums go to `partial`, [split][M][N].
+template <bool BF, bool AA, bool BA, int WM, int WN, int MF>
+__global__ __launch_bounds__(WM* WN* kWave, 2) void k_product(const char* a, int64_t a_ld, const char* b, int64_t b_ld, void* c, int64_t c_ld,
+                                                             int64_t M, int64_t N, int64_t K, int64_t tiles_m, int64_t tiles_n,
+                                                             int64_t steps_each, float* partial, int vec, Epilogue ep) {
+    typedef Shape<BF, AA, BA, WM, WN, MF> S;
+    typedef typename S::A A;
+    typedef typename S::B B;
+    extern __shared__ __attribute__((aligned(16))) char lds_raw[];
+    lds_char* const lds = (lds_char*)lds_raw;
+    constexpr int kBuf = A::kBytes + B::kBytes;
+    int64_t tm, tn;
+    const int64_t tiles = tiles_m * tiles_n, split = blockIdx.x / tiles;
+    tile_of(blockIdx.x - split * tiles, tiles, tiles_m, tiles_n, tm, tn);
+    const int64_t i0 = tm * S::BM, j0 = tn * S::BN;
+    const int64_t all = (K + A::kStep - 1) / A::kStep, s0 = split * steps_each, s1 = s0 + steps_each < all ? s0 + steps_each : all;
+    const bool cut = s1 == all && K % A::kStep != 0;   // the last step of this split ends inside
+    const int64_t whole = s1 - cut;
+
+    unsigned a_off[A::kLoads], b_off[B::kLoads];
+    A::sources(a_off, a_ld, M - i0);
+    B::sources(b_off, b_ld, N - j0);
+    const char* ap = a + (AA ? i0 * a_ld : i0) * S::Z + s0 * A::step_bytes(a_ld);
+    const char* bp = b + (BA ? j0 * b_ld : j0) * S::Z + s0 * B::step_bytes(b_ld);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), wm = wave / WN, wn = wave % WN;
+
+    v4f acc[MF][4];
+#pragma unroll
+    for (int m = 0; m < MF; ++m)
+#pragma unroll
+        for (int n = 0; n < 4; ++n) acc[m][n] = v4f{0.f, 0.f, 0.f, 0.f};
+
+    auto fetch = [&](int64_t s, int buf) {   // step s to LDS
+        lds_char* to = lds + buf * kBuf;
+        if (s < whole) {
+            A::load(ap, a_off, to);
+            B::load(bp, b_off, to + A::kBytes);
+        } else {
+            const int left = (int)(K - s * A::kStep);
+            A::load_cut(ap, a_off, to, left);
+            B::load_cut(bp, b_off, to + A::kBytes, left);
+        }
+        ap += A::step_bytes(a_ld);
+        bp += B::step_bytes(b_ld);
+    };
+    auto multiply = [&](int buf) {
+        const lds_char *as = lds + buf * kBuf, *bs = as + A::kBytes;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            if constexpr (BF) {
+                v8bf x[MF], y[4];
+#pragma unroll
+                for (int n = 0; n < 4; ++n) y[n] = B::frag16(bs, wn * 64, n, h);
+#pragma unroll
+                for (int m = 0; m < MF; ++m) x[m] = A::frag16(as, wm * MF * 16, m, h);
+#pragma unroll
+                for (int m = 0; m < MF; ++m)
+#pragma unroll
+                    for (int n = 0; n < 4; ++n) acc[m][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(y[n], x[m], acc[m][n], 0, 0, 0);
+            } else {
+                v4f x[MF], y[4];
+#pragma unroll
+                for (int n = 0; n < 4; ++n) y[n] = B::frag32(bs, wn * 64, n, h);
+#pragma unroll
+                for (int m = 0; m < MF; ++m) x[m] = A::frag32(as, wm * MF * 16, m, h);
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+#pragma unroll
+                    for (int m = 0; m < MF; ++m)
+#pragma unroll
+                        for (int n = 0; n < 4; ++n) acc[m][n] = __builtin_amdgcn_mfma_f32_16x16x4f32(y[n][e], x[m][e], acc[m][n], 0, 0, 0);
+            }
+        }
+    };
+
+    if (s0 < s1) {
+        fetch(s0, 0);
+        int buf = 0;
+        for (int64_t s = s0; s < s1; ++s, buf ^= 1) {
+            __builtin_amdgcn_s_waitcnt(kLanded);
+            __syncthreads();   // this step's loads have landed, the other half is read
+            if (s + 1 < s1) fetch(s + 1, buf ^ 1);
+            multiply(buf);
+        }
+    }
+
+    // 64 x 64 sums of a wave: row r holds its sixteen quads in the order q ^ (r & 15)
+    __syncthreads();
+    const int lane = threadIdx.x & 63, g = lane >> 4;
+    lds_char* const mine = lds + wave * 16384;
+    const int64_t j = j0 + wn * 64 + 8 * (lane & 7);
+    Draw d{};
+    float bias[8] = {};
+    if (!partial) {
+        if (ep.drop.below) d = make_draw(ep.drop.rng, ep.drop.offset);
+        bias_oct(ep, j, N, bias);
+    }
+#pragma unroll
+    for (int part = 0; part < MF / 4; ++part) {
+#pragma unroll
+        for (int m = 0; m < 4; ++m)
+#pragma unroll
+            for (int n = 0; n < 4; ++n)
+                *reinterpret_cast<__attribute__((address_space(3))) v4f*>(mine + (16 * m + (lane & 15)) * 256 + (((4 * n + g) ^ (lane & 15)) << 4)) =
+                    acc[4 * part + m][n];
+        const int64_t i1 = i0 + wm * MF * 16 + 64 * part;
+#pragma unroll 1
+        for (int r = lane >> 3; r < 64; r += 8) {
+            const int64_t i = i1 + r;
+            if (i >= M || j >= N) break;
+            float sum[8];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const v4f t = *reinterpret_cast<const __attribute__((address_space(3))) v4f*>(mine + r * 256 + (((2 * (lane & 7) + h) ^ (r & 15)) << 4));
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sum[4 * h + e] = t[e];
+            }
+            if (partial) st_oct<false>(partial, (split * M + i) * N + j, N - j < 8 ? (int)(N - j) : 8, N % 4 == 0 && N - j >= 8, sum);
+            else finish_oct<BF>(ep, d, c, c_ld, i, j, N, sum, bias, vec);
+        }
+    }
+}
+
+// The sum over the splits, in order, and the epilogue.  One lane: eight columns.
+template <bool BF>
+__global__ __launch_bounds__(kBlock) void k_join(const float* partial, int64_t splits, void* c, int64_t c_ld, int64_t M, int64_t N, int vec,
+                                                 Epilogue ep) {
+    const int64_t per_row = (N + 7) / 8, at = (int64_t)blockIdx.x * kBlock + threadIdx.x;
+    Draw d{};
+    if (ep.drop.below) d = make_draw(ep.drop.rng, ep.drop.offset);
+    if (at >= M * per_row) return;
+    const int64_t i = at / per_row, j = 8 * (at - i * per_row);
+    const int count = N - j < 8 ? (int)(N - j) : 8;
+    float v[8] = {}, bias[8];
+    bias_oct(ep, j, N, bias);
+    for (int64_t s = 0; s < splits; ++s) {
+        float x[8];
+        ld_oct<false>(partial, (s * M + i) * N + j, count, N % 4 == 0 && count == 8, x);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] += x[e];
+    }
+    finish_oct<BF>(ep, d, c, c_ld, i, j, N, v, bias, vec);
+}
+
+namespace {
+
+constexpr int kCUs = 256;
+
+struct Choice {
+    bool big;          // tiles of 256 x 256 (bf16), else 128 x 128
+    int64_t splits, steps_each, tiles_m, tiles_n;
+};
+
+Choice choose(bool bf16, int64_t M, int64_t N, int64_t K) {
+    Choice c{};
+    const int64_t steps = (K + (bf16 ? 63 : 31)) / (bf16 ? 64 : 32);
+    const int64_t t256 = ((M + 255) / 256) * ((N + 255) / 256);
+    c.big = bf16 && t256 >= kCUs;
+    const int64_t side = c.big ? 256 : 128;
+    c.tiles_m = (M + side - 1) / side;
+    c.tiles_n = (N + side - 1) / side;
+    const int64_t tiles = c.tiles_m * c.tiles_n;
+    c.splits = std::max<int64_t>(1, std::min<int64_t>(kCUs / std::max<int64_t>(tiles, 1), steps / 8));
+    c.steps_each = std::max<int64_t>(1, (steps + c.splits - 1) / c.splits);
+    c.splits = std::max<int64_t>(1, (steps + c.steps_each - 1) / c.steps_each);
+    return c;
+}
+
+template <bool BF, bool AA, bool BA, int WM, int WN, int MF>
+hipError_t start(const ProductCall& p, const Choice& ch, int vec) {
+    typedef Shape<BF, AA, BA, WM, WN, MF> S;
+    auto k = k_product<BF, AA, BA, WM, WN, MF>;
+    if (S::kLds > 65536) {
+        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(k), hipFuncAttributeMaxDynamicSharedMemorySize, S::kLds);
+        if (e != hipSuccess) return e;
+    }
+    hipLaunchKernelGGL(k, dim3((unsigned)(ch.tiles_m * ch.tiles_n * ch.splits)), dim3(S::T), S::kLds, p.stream, static_cast<const char*>(p.a), p.a_ld,
+                       static_cast<const char*>(p.b), p.b_ld, p.c, p.c_ld, p.M, p.N, p.K, ch.tiles_m, ch.tiles_n, ch.steps_each,
+                       ch.splits > 1 ? p.partial : nullptr, vec, epilogue_of(p.ep));
+    return hipGetLastError();
+}
+
+template <bool BF, int WM, int WN, int MF>
+hipError_t start_by_order(const ProductCall& p, const Choice& ch, int vec) {
+    if (p.a_along) return p.b_along ? start<BF, true, true, WM, WN, MF>(p, ch, vec) : start<BF, true, false, WM, WN, MF>(p, ch, vec);
+    return start<BF, false, false, WM, WN, MF>(p, ch, vec);
+}
+
+bool vec_aligned(const void* p, int64_t ld, int64_t z) { return !p || (reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld * z % 16 == 0); }
+
+}  // namespace
+
+int64_t product_partial_bytes(bool bf16, int64_t M, int64_t N, int64_t K) {
+    // the most of any smaller M too (a program sizes its workspace once, for its longest batch)
+    int64_t most = 0;
+    for (int64_t m = std::min<int64_t>(M, 128);; m = std::min<int64_t>(M, m + 128)) {
+        const Choice ch = choose(bf16, m, N, K);
+        if (ch.splits > 1) most = std::max(most, ch.splits * m * N * 4);
+        if (m >= M || m / 128 >= kCUs) break;
+    }
+    return most;
+}
+
+psgd_status launch_product(const ProductCall& p, std::string* what) {
+    const Choice ch = choose(p.bf16, p.M, p.N, p.K);
+    const int64_t z = p.bf16 ? 2 : 4;
+    if (ch.tiles_m * ch.tiles_n * ch.splits > 0x7fffffffLL) return PSGD_EUNSUPPORTED;
+    const int vec = vec_aligned(p.c, p.c_ld, z) && vec_aligned(p.ep.pre, p.ep.pre_ld, z) && vec_aligned(p.ep.residual, p.ep.residual_ld, z);
+    hipError_t e;
+    if (!p.bf16) e = start_by_order<false, 2, 2, 4>(p, ch, vec);
+    else if (ch.big) e = start_by_order<true, 2, 4, 8>(p, ch, vec);
+    else e = start_by_order<true, 2, 2, 4>(p, ch, vec);
+    if (e != hipSuccess) { *what = std::string("launch k_product: ") + hipGetErrorString(e); return PSGD_EHIP; }
+    if (ch.splits > 1) {
+        const int64_t blocks = (p.M * ((p.N + 7) / 8) + kBlock - 1) / kBlock;
+        auto k = p.bf16 ? k_join<true> : k_join<false>;
+        hipLaunchKernelGGL(k, dim3((unsigned)blocks), dim3(kBlock), 0, p.stream, p.partial, ch.splits, p.c, p.c_ld, p.M, p.N, vec, epilogue_of(p.ep));
+        e = hipGetLastError();
+        if (e != hipSuccess) { *what = std::string("launch k_join: ") + hipGetErrorString(e); return PSGD_EHIP; }
+    }
+    return PSGD_OK;
+}
+
+}  // namespace psgd
