@@ -2,57 +2,57 @@
 #include <hip/hip_runtime.h>
 
 #include <string>
+#include <type_traits>
 
-#include "psgd_device.h"
-#include "psgd_operators.h"
-#include "psgd_random.h"
+#include "psgd_epilogue.h"
 
 namespace psgd {
 
-template <bool BF>
-__device__ __forceinline__ float ld_elem(const void* p, int64_t at) {
-    if constexpr (BF) return bf16_to_f32(static_cast<const bf16_t*>(p)[at]);
-    else return static_cast<const float*>(p)[at];
-}
-template <bool BF>
-__device__ __forceinline__ void st_elem(void* p, int64_t at, float v) {
-    if constexpr (BF) static_cast<bf16_t*>(p)[at] = f32_to_bf16(v);
-    else static_cast<float*>(p)[at] = v;
-}
+// y = residual + D(x).  One lane: eight consecutive columns of a row, one call of the generator.  A workgroup: `high` rows of a band of
+// `wide` groups of eight columns, about kDropItems of them; which row an item lies in is a multiplication (recip =
+// ceil(2^32 / wide), 0 for one group; exact below 2^16 items).
+constexpr int kDropItems = 1024;
 
-// y = residual + D(x).  One lane: eight consecutive columns of one row (one call of the generator).
 template <bool BF>
 __global__ __launch_bounds__(kBlock) void k_dropout(const void* x, int64_t x_ld, const void* residual, int64_t residual_ld, void* y,
-                                                    int64_t y_ld, int64_t rows, int64_t cols, DropArgs drop) {
-    const int64_t groups = (cols + 7) / 8;
-    const int64_t at = (int64_t)blockIdx.x * kBlock + threadIdx.x;
+                                                    int64_t y_ld, int64_t rows, int64_t cols, int wide, int high, unsigned recip,
+                                                    int64_t bands, DropArgs drop) {
+    const int64_t strip = blockIdx.x / bands, g0 = (blockIdx.x - strip * bands) * wide, row0 = strip * high;
+    const int n = (int)(rows - row0 < high ? rows - row0 : high) * wide;
     Draw d{};
     if (drop.below) d = make_draw(drop.rng, drop.offset);
-    if (at >= rows * groups) return;
-    const int64_t row = at / groups, g = at - row * groups;
-    Words r{};
-    if (drop.below) r = philox(d, (unsigned)g, (unsigned)row);
-    for (int j = 0; j < 8; ++j) {
-        const int64_t col = 8 * g + j;
-        if (col >= cols) break;
-        float v = dropped(r, j, drop.below) ? 0.f : ld_elem<BF>(x, row * x_ld + col) * drop.factor;
-        if (residual) v += ld_elem<BF>(residual, row * residual_ld + col);
-        st_elem<BF>(y, row * y_ld + col, v);
+    for (int item = threadIdx.x; item < n; item += kBlock) {
+        const int r = recip ? (int)__umulhi((unsigned)item, recip) : item;
+        const int64_t row = row0 + r, col = 8 * (g0 + item - r * wide);
+        const int count = (int)(cols - col < 8 ? cols - col : 8);
+        if (count <= 0) continue;
+        float v[8];
+        ld_oct<BF>(x, row * x_ld + col, count, v);
+        if (drop.below) {
+            const Words w = philox(d, (unsigned)(col >> 3), (unsigned)row);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = dropped(w, e, drop.below) ? 0.f : v[e] * drop.factor;
+        }
+        if (residual) {
+            float z[8];
+            ld_oct<BF>(residual, row * residual_ld + col, count, z);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] += z[e];
+        }
+        st_oct<BF>(y, row * y_ld + col, count, v);
     }
 }
 
 psgd_status launch_dropout(const DropoutCall& c, std::string* what) {
-    const int64_t lanes = c.rows * ((c.cols + 7) / 8);
-    const int64_t blocks = (lanes + kBlock - 1) / kBlock;
+    const int64_t groups = (c.cols + 7) / 8;
+    const int wide = (int)(groups < kDropItems ? groups : kDropItems);
+    const int high = wide < kDropItems ? kDropItems / wide : 1;
+    const unsigned recip = wide > 1 ? (unsigned)(((uint64_t(1) << 32) + wide - 1) / wide) : 0;
+    const int64_t bands = (groups + wide - 1) / wide, blocks = (c.rows + high - 1) / high * bands;
     if (blocks > 0x7fffffffLL) return PSGD_EUNSUPPORTED;
-    DropArgs d;
-    d.rng = c.drop.rng;
-    d.offset = c.drop.offset;
-    d.below = c.drop.below;
-    d.factor = c.drop.factor;
     auto k = c.bf16 ? k_dropout<true> : k_dropout<false>;
     hipLaunchKernelGGL(k, dim3((unsigned)blocks), dim3(kBlock), 0, static_cast<hipStream_t>(c.stream), c.x, c.x_ld, c.residual,
-                       c.residual_ld, c.y, c.y_ld, c.rows, c.cols, d);
+                       c.residual_ld, c.y, c.y_ld, c.rows, c.cols, wide, high, recip, bands, drop_of(c.drop));
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) { *what = std::string("launch k_dropout: ") + hipGetErrorString(e); return PSGD_EHIP; }
     return PSGD_OK;
@@ -60,10 +60,29 @@ psgd_status launch_dropout(const DropoutCall& c, std::string* what) {
 
 // ---- random mask ---------------------------------------------------------------------------------------------------
 
+// Four consecutive entries of the gradient, read once, and of Delta', written once
+template <bool BF>
+__device__ __forceinline__ v4f ld_grad4(const void* p, int64_t at) {
+    if constexpr (BF) {
+        const v2u t = __builtin_nontemporal_load(reinterpret_cast<const v2u*>(static_cast<const bf16_t*>(p) + at));
+        return v4f{__uint_as_float(t.x << 16), __uint_as_float(t.x & 0xffff0000u), __uint_as_float(t.y << 16), __uint_as_float(t.y & 0xffff0000u)};
+    } else {
+        return __builtin_nontemporal_load(reinterpret_cast<const v4f*>(static_cast<const float*>(p) + at));
+    }
+}
+template <bool BF>
+__device__ __forceinline__ void st_out4(void* p, int64_t at, v4f v) {
+    if constexpr (BF)
+        __builtin_nontemporal_store(v2u{pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w)}, reinterpret_cast<v2u*>(static_cast<bf16_t*>(p) + at));
+    else __builtin_nontemporal_store(v, reinterpret_cast<v4f*>(static_cast<float*>(p) + at));
+}
+
 // blockIdx.x: a slice of kFlatTileElems elements (as k_ef_add_zero's); one lane: four consecutive entries of one matrix and
 // all workers.  Entry `pos` of tensor t takes word pos % 4 of the counter (pos / 4, t) and is kept where it is below
-// `threshold`, or, with threshold 0 given, below the share of the entries that the plan's budget is.
-template <bool GBF, bool OBF>
+// `threshold`, or, with `budget`, below the share of the entries that the plan keeps.  Up to CAP workers' M stay in registers from
+// the mean to the new error memory, so every element moves once; with more (CAP = 0) M is written, and the lanes that keep
+// something read theirs again.
+template <bool GBF, bool OBF, int CAP>
 __global__ __launch_bounds__(kBlock) void k_random_mask(const MatDesc* __restrict__ mats, const int64_t* __restrict__ first, int n_mats,
                                                         const void* __restrict__ grad, float* __restrict__ err, void* __restrict__ out,
                                                         int workers, int64_t gstride, int64_t estride, int64_t n_mat_elems,
@@ -77,8 +96,8 @@ __global__ __launch_bounds__(kBlock) void k_random_mask(const MatDesc* __restric
         const int64_t e1 = e0 + kFlatTileElems < n_vec_elems ? e0 + kFlatTileElems : n_vec_elems;
         for (int64_t idx = e0 + threadIdx.x; idx < e1; idx += kBlock) {
             float s = 0.f;
-            for (int w = 0; w < workers; ++w) s += ld_elem<GBF>(grad, (int64_t)w * gstride + n_mat_elems + idx);
-            st_elem<OBF>(out, n_mat_elems + idx, s * inv_w);
+            for (int w = 0; w < workers; ++w) s += ld_any(grad, (int64_t)w * gstride + n_mat_elems + idx, GBF);
+            st_any(out, n_mat_elems + idx, s * inv_w, OBF);
         }
         return;
     }
@@ -91,19 +110,61 @@ __global__ __launch_bounds__(kBlock) void k_random_mask(const MatDesc* __restric
     const MatDesc d = mats[lo];
     const int64_t nm = (int64_t)d.n * d.m;
     const int64_t pos = (slice - first[lo]) * kFlatTileElems + 4 * threadIdx.x;
+    if (pos >= nm) return;
+    const int64_t at = d.off + pos;
     const uint64_t below = budget ? ((uint64_t)d.kept << 32) / (uint64_t)nm : threshold;
+    if (pos + 4 <= nm) {   // matrices start on multiples of 64 elements: aligned
+        v4f sum = v4f{0.f, 0.f, 0.f, 0.f};
+        constexpr int kHeld = CAP > 0 ? CAP : 1;
+        v4f m[kHeld];
+        if constexpr (CAP > 0) {
+#pragma unroll
+            for (int w = 0; w < CAP; ++w)
+                if (w < workers) m[w] = ld_grad4<GBF>(grad, w * gstride + at) + *reinterpret_cast<const v4f*>(err + w * estride + at);
+#pragma unroll
+            for (int w = 0; w < CAP; ++w)
+                if (w < workers) sum += m[w];
+        } else {
+            for (int w = 0; w < workers; ++w) {
+                v4f* e = reinterpret_cast<v4f*>(err + w * estride + at);
+                const v4f t = ld_grad4<GBF>(grad, w * gstride + at) + *e;
+                *e = t;
+                sum += t;
+            }
+        }
+        const Words r = philox(make_draw(rng, offset), (unsigned)(pos >> 2), (unsigned)d.tensor);
+        v4f delta;
+        bool any = false;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const bool keep = r.w[j] < below;
+            any |= keep;
+            delta[j] = keep ? sum[j] * inv_w : 0.f;
+        }
+        if constexpr (CAP > 0) {
+#pragma unroll
+            for (int w = 0; w < CAP; ++w)
+                if (w < workers) *reinterpret_cast<v4f*>(err + w * estride + at) = m[w] - delta;
+        } else if (any) {
+            for (int w = 0; w < workers; ++w) {
+                v4f* e = reinterpret_cast<v4f*>(err + w * estride + at);
+                *e = *e - delta;
+            }
+        }
+        st_out4<OBF>(out, at, delta);
+        return;
+    }
     const Words r = philox(make_draw(rng, offset), (unsigned)(pos >> 2), (unsigned)d.tensor);
-    for (int j = 0; j < 4; ++j) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {   // a matrix's last one to three entries
         if (pos + j >= nm) break;
-        const int64_t at = d.off + pos + j;
-        const bool keep = r.w[j] < below;
         float s = 0.f;
-        for (int w = 0; w < workers; ++w) s += ld_elem<GBF>(grad, (int64_t)w * gstride + at) + err[(int64_t)w * estride + at];
-        const float delta = keep ? s * inv_w : 0.f;
-        st_elem<OBF>(out, at, delta);
+        for (int w = 0; w < workers; ++w) s += ld_any(grad, w * gstride + at + j, GBF) + err[w * estride + at + j];
+        const float delta = r.w[j] < below ? s * inv_w : 0.f;
+        st_any(out, at + j, delta, OBF);
         for (int w = 0; w < workers; ++w) {
-            const float m = ld_elem<GBF>(grad, (int64_t)w * gstride + at) + err[(int64_t)w * estride + at];
-            err[(int64_t)w * estride + at] = keep ? m - delta : m;
+            float* e = err + w * estride + at + j;
+            *e = ld_any(grad, w * gstride + at + j, GBF) + *e - delta;
         }
     }
 }
@@ -127,8 +188,13 @@ psgd_status launch_random_mask(psgd_plan* plan, const void* grad, float* err, do
     if (slices == 0) return PSGD_OK;
     const uint64_t threshold = keep < 0 ? 0 : (uint64_t)(keep * 4294967296.0 + 0.5);
     const bool gbf = plan->grad_dtype == PSGD_BF16, obf = plan->out_dtype == PSGD_BF16;
-    auto k = gbf ? (obf ? k_random_mask<true, true> : k_random_mask<true, false>)
-                 : (obf ? k_random_mask<false, true> : k_random_mask<false, false>);
+    auto by_workers = [&](auto g, auto o) {
+        constexpr bool G = decltype(g)::value, O = decltype(o)::value;
+        return plan->workers == 1 ? k_random_mask<G, O, 1> : plan->workers <= 4 ? k_random_mask<G, O, 4>
+             : plan->workers <= 16 ? k_random_mask<G, O, 16> : k_random_mask<G, O, 0>;
+    };
+    auto k = gbf ? (obf ? by_workers(std::true_type(), std::true_type()) : by_workers(std::true_type(), std::false_type()))
+                 : (obf ? by_workers(std::false_type(), std::true_type()) : by_workers(std::false_type(), std::false_type()));
     hipLaunchKernelGGL(k, dim3((unsigned)slices), dim3(kBlock), 0, static_cast<hipStream_t>(stream), plan->dev.mats,
                        plan->dev.flat_first, (int)plan->mats.size(), grad, err, out, plan->workers, plan->sizes.grad_stride,
                        plan->sizes.err_stride, plan->sizes.n_mat_elems, plan->sizes.n_vec_elems, keep < 0 ? 1 : 0, threshold, rng, offset);

@@ -70,16 +70,22 @@ inline Epilogue epilogue_of(const EpilogueHost& h) {
     return Epilogue{h.scale, h.bias, h.bias_bf, h.act, h.pre, h.pre_ld, h.residual, h.residual_ld, drop_of(h.drop)};
 }
 
-// Eight consecutive elements of a row; `vec`: all exist and lie on a multiple of sixteen bytes
+// Sixteen bytes that begin anywhere an element may: this generation's global accesses need no more than that, so rows of odd
+// lengths and views that start anywhere take the same wide accesses.
+typedef unsigned v4u_any __attribute__((ext_vector_type(4), aligned(2)));
+typedef float v4f_any __attribute__((ext_vector_type(4), aligned(4)));
+
+// Eight consecutive elements of a row, `count` of which exist
 template <bool BF>
-__device__ __forceinline__ void ld_oct(const void* p, int64_t at, int count, bool vec, float (&x)[8]) {
-    if (vec) {
+__device__ __forceinline__ void ld_oct(const void* p, int64_t at, int count, float (&x)[8]) {
+    if (count >= 8) {
         if constexpr (BF) {
-            const v4u t = *reinterpret_cast<const v4u*>(static_cast<const bf16_t*>(p) + at);
+            const v4u t = *reinterpret_cast<const v4u_any*>(static_cast<const bf16_t*>(p) + at);
 #pragma unroll
             for (int e = 0; e < 4; ++e) { x[2 * e] = __uint_as_float(t[e] << 16); x[2 * e + 1] = __uint_as_float(t[e] & 0xffff0000u); }
         } else {
-            const v4f lo = *reinterpret_cast<const v4f*>(static_cast<const float*>(p) + at), hi = *reinterpret_cast<const v4f*>(static_cast<const float*>(p) + at + 4);
+            const v4f lo = *reinterpret_cast<const v4f_any*>(static_cast<const float*>(p) + at);
+            const v4f hi = *reinterpret_cast<const v4f_any*>(static_cast<const float*>(p) + at + 4);
 #pragma unroll
             for (int e = 0; e < 4; ++e) { x[e] = lo[e]; x[4 + e] = hi[e]; }
         }
@@ -89,14 +95,14 @@ __device__ __forceinline__ void ld_oct(const void* p, int64_t at, int count, boo
     }
 }
 template <bool BF>
-__device__ __forceinline__ void st_oct(void* p, int64_t at, int count, bool vec, const float (&x)[8]) {
-    if (vec) {
+__device__ __forceinline__ void st_oct(void* p, int64_t at, int count, const float (&x)[8]) {
+    if (count >= 8) {
         if constexpr (BF) {
-            *reinterpret_cast<v4u*>(static_cast<bf16_t*>(p) + at) =
+            *reinterpret_cast<v4u_any*>(static_cast<bf16_t*>(p) + at) =
                 v4u{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7])};
         } else {
-            *reinterpret_cast<v4f*>(static_cast<float*>(p) + at) = v4f{x[0], x[1], x[2], x[3]};
-            *reinterpret_cast<v4f*>(static_cast<float*>(p) + at + 4) = v4f{x[4], x[5], x[6], x[7]};
+            *reinterpret_cast<v4f_any*>(static_cast<float*>(p) + at) = v4f{x[0], x[1], x[2], x[3]};
+            *reinterpret_cast<v4f_any*>(static_cast<float*>(p) + at + 4) = v4f{x[4], x[5], x[6], x[7]};
         }
     } else {
 #pragma unroll
@@ -114,13 +120,12 @@ __device__ __forceinline__ void bias_oct(const Epilogue& ep, int64_t j, int64_t 
 // Columns j .. j + 7 (j a multiple of eight) of row i from their sums: one call of the generator.
 template <bool BF>
 __device__ __forceinline__ void finish_oct(const Epilogue& ep, const Draw& d, void* c, int64_t c_ld, int64_t i, int64_t j, int64_t N,
-                                           const float (&sum)[8], const float (&bias)[8], bool vec) {
+                                           const float (&sum)[8], const float (&bias)[8]) {
     const int count = N - j < 8 ? (int)(N - j) : 8;
-    vec = vec && count == 8;
     float v[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = sum[e] * ep.scale + bias[e];
-    if (ep.pre) st_oct<BF>(ep.pre, i * ep.pre_ld + j, count, vec, v);
+    if (ep.pre) st_oct<BF>(ep.pre, i * ep.pre_ld + j, count, v);
     if (ep.act != PSGD_ACT_IDENTITY)
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = act_of(v[e], ep.act);
@@ -131,11 +136,11 @@ __device__ __forceinline__ void finish_oct(const Epilogue& ep, const Draw& d, vo
     }
     if (ep.residual) {
         float x[8];
-        ld_oct<BF>(ep.residual, i * ep.residual_ld + j, count, vec, x);
+        ld_oct<BF>(ep.residual, i * ep.residual_ld + j, count, x);
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] += x[e];
     }
-    st_oct<BF>(c, i * c_ld + j, count, vec, v);
+    st_oct<BF>(c, i * c_ld + j, count, v);
 }
 
 }  // namespace psgd

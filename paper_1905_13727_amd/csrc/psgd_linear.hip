@@ -12,16 +12,15 @@ namespace psgd {
 // dst [rows][dst_ld] = src [rows][cols], rounded if dst is bf16 and src is not; columns up to dst_ld are zero.
 // One lane: eight columns.
 template <bool SBF, bool DBF>
-__global__ __launch_bounds__(kBlock) void k_lay_out(const void* src, int64_t src_ld, void* dst, int64_t dst_ld, int64_t rows, int64_t cols,
-                                                    int vec) {
+__global__ __launch_bounds__(kBlock) void k_lay_out(const void* src, int64_t src_ld, void* dst, int64_t dst_ld, int64_t rows, int64_t cols) {
     const int64_t per_row = (dst_ld + 7) / 8, at = (int64_t)blockIdx.x * kBlock + threadIdx.x;
     if (at >= rows * per_row) return;
     const int64_t row = at / per_row, j = 8 * (at - row * per_row);
     float x[8];
     const int count = cols - j < 8 ? (int)(cols - j) : 8;
-    ld_oct<SBF>(src, row * src_ld + j, count, vec && count == 8, x);
+    ld_oct<SBF>(src, row * src_ld + j, count, x);
     const int to = dst_ld - j < 8 ? (int)(dst_ld - j) : 8;
-    st_oct<DBF>(dst, row * dst_ld + j, to, to == 8, x);
+    st_oct<DBF>(dst, row * dst_ld + j, to, x);
 }
 
 // dz = D(dy) act'(pre) without the factor of the elements that stay, which goes into the products' epilogues: where the
@@ -31,24 +30,23 @@ constexpr int kDzRows = 64;
 
 template <bool BF>
 __global__ __launch_bounds__(kBlock) void k_dz(const void* dy, int64_t dy_ld, const void* pre, int64_t pre_ld, int act, DropArgs drop,
-                                               void* dz, int64_t dz_ld, float* partial, int64_t T, int64_t n, int vec) {
+                                               void* dz, int64_t dz_ld, float* partial, int64_t T, int64_t n) {
     __shared__ float sums[8][264];
     const int lane_c = threadIdx.x & 31, lane_t = threadIdx.x >> 5;
     const int64_t blocks_c = (n + 255) / 256, bt = blockIdx.x / blocks_c, bc = blockIdx.x - bt * blocks_c;
     const int64_t c0 = bc * 256 + 8 * lane_c;
     const int64_t t0 = bt * kDzRows, t1 = t0 + kDzRows < T ? t0 + kDzRows : T;
     const int count = n - c0 < 8 ? (int)(n - c0) : 8;
-    const bool whole = vec && count == 8;
     Draw d{};
     if (drop.below) d = make_draw(drop.rng, drop.offset);
     float s[8] = {};
     if (count > 0) {
         for (int64_t t = t0 + lane_t; t < t1; t += 8) {
             float v[8];
-            ld_oct<BF>(dy, t * dy_ld + c0, count, whole, v);
+            ld_oct<BF>(dy, t * dy_ld + c0, count, v);
             if (act != PSGD_ACT_IDENTITY) {
                 float z[8];
-                ld_oct<BF>(pre, t * pre_ld + c0, count, whole, z);
+                ld_oct<BF>(pre, t * pre_ld + c0, count, z);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) v[j] *= act_slope(z[j], act);
             }
@@ -62,7 +60,7 @@ __global__ __launch_bounds__(kBlock) void k_dz(const void* dy, int64_t dy_ld, co
 #pragma unroll
                     for (int j = 0; j < 8; ++j) v[j] = j < count ? v[j] : 0.f;
                 const int to = dz_ld - c0 < 8 ? (int)(dz_ld - c0) : 8;
-                st_oct<BF>(dz, t * dz_ld + c0, to, to == 8, v);
+                st_oct<BF>(dz, t * dz_ld + c0, to, v);
             }
 #pragma unroll
             for (int j = 0; j < 8; ++j) s[j] += v[j];
@@ -136,9 +134,8 @@ Parts parts_of(const LinearCall& c) {
 bool lay_out(const void* src, int64_t src_ld, bool src_bf, void* dst, int64_t dst_ld, bool dst_bf, int64_t rows, int64_t cols, hipStream_t s,
              std::string* what) {
     const int64_t blocks = (rows * ((dst_ld + 7) / 8) + kBlock - 1) / kBlock;
-    const int vec = vec_aligned(src, src_ld, src_bf ? 2 : 4);
     auto k = src_bf ? k_lay_out<true, true> : dst_bf ? k_lay_out<false, true> : k_lay_out<false, false>;
-    hipLaunchKernelGGL(k, dim3((unsigned)blocks), dim3(kBlock), 0, s, src, src_ld, dst, dst_ld, rows, cols, vec);
+    hipLaunchKernelGGL(k, dim3((unsigned)blocks), dim3(kBlock), 0, s, src, src_ld, dst, dst_ld, rows, cols);
     return !failed("k_lay_out", what);
 }
 
@@ -207,10 +204,9 @@ psgd_status launch_linear_backward(const LinearCall& c, std::string* what) {
         }
         if (!direct || c.db) {
             auto k = c.bf16 ? k_dz<true> : k_dz<false>;
-            const int vec = vec_aligned(c.dy, c.dy_ld, z) && (c.act == PSGD_ACT_IDENTITY || vec_aligned(c.pre, c.pre_ld, z));
             if ((c.n + 255) / 256 * blocks > 0x7fffffffLL) return PSGD_EUNSUPPORTED;
             hipLaunchKernelGGL(k, dim3((unsigned)((c.n + 255) / 256 * blocks)), dim3(kBlock), 0, s, c.dy, c.dy_ld, c.pre, c.pre_ld, c.act, drop_of(c.drop),
-                               direct ? nullptr : const_cast<void*>(dz), dz_ld, c.db ? reinterpret_cast<float*>(ws + p.db) : nullptr, c.T, c.n, vec);
+                               direct ? nullptr : const_cast<void*>(dz), dz_ld, c.db ? reinterpret_cast<float*>(ws + p.db) : nullptr, c.T, c.n);
             if (failed("k_dz", what)) return PSGD_EHIP;
         }
     }

@@ -145,7 +145,7 @@ struct Shape {   // WM x WN waves, each MF x 4 fragments of 16 x 16
 template <bool BF, bool AA, bool BA, int WM, int WN, int MF>
 __global__ __launch_bounds__(WM* WN* kWave, 2) void k_product(const char* a, int64_t a_ld, const char* b, int64_t b_ld, void* c, int64_t c_ld,
                                                              int64_t M, int64_t N, int64_t K, int64_t tiles_m, int64_t tiles_n,
-                                                             int64_t steps_each, float* partial, int vec, Epilogue ep) {
+                                                             int64_t steps_each, float* partial, Epilogue ep) {
     typedef Shape<BF, AA, BA, WM, WN, MF> S;
     typedef typename S::A A;
     typedef typename S::B B;
@@ -258,15 +258,15 @@ __global__ __launch_bounds__(WM* WN* kWave, 2) void k_product(const char* a, int
 #pragma unroll
                 for (int e = 0; e < 4; ++e) sum[4 * h + e] = t[e];
             }
-            if (partial) st_oct<false>(partial, (split * M + i) * N + j, N - j < 8 ? (int)(N - j) : 8, N % 4 == 0 && N - j >= 8, sum);
-            else finish_oct<BF>(ep, d, c, c_ld, i, j, N, sum, bias, vec);
+            if (partial) st_oct<false>(partial, (split * M + i) * N + j, N - j < 8 ? (int)(N - j) : 8, sum);
+            else finish_oct<BF>(ep, d, c, c_ld, i, j, N, sum, bias);
         }
     }
 }
 
 // The sum over the splits, in order, and the epilogue.  One lane: eight columns.
 template <bool BF>
-__global__ __launch_bounds__(kBlock) void k_join(const float* partial, int64_t splits, void* c, int64_t c_ld, int64_t M, int64_t N, int vec,
+__global__ __launch_bounds__(kBlock) void k_join(const float* partial, int64_t splits, void* c, int64_t c_ld, int64_t M, int64_t N,
                                                  Epilogue ep) {
     const int64_t per_row = (N + 7) / 8, at = (int64_t)blockIdx.x * kBlock + threadIdx.x;
     Draw d{};
@@ -278,11 +278,11 @@ __global__ __launch_bounds__(kBlock) void k_join(const float* partial, int64_t s
     bias_oct(ep, j, N, bias);
     for (int64_t s = 0; s < splits; ++s) {
         float x[8];
-        ld_oct<false>(partial, (s * M + i) * N + j, count, N % 4 == 0 && count == 8, x);
+        ld_oct<false>(partial, (s * M + i) * N + j, count, x);
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] += x[e];
     }
-    finish_oct<BF>(ep, d, c, c_ld, i, j, N, v, bias, vec);
+    finish_oct<BF>(ep, d, c, c_ld, i, j, N, v, bias);
 }
 
 namespace {
@@ -310,7 +310,7 @@ Choice choose(bool bf16, int64_t M, int64_t N, int64_t K) {
 }
 
 template <bool BF, bool AA, bool BA, int WM, int WN, int MF>
-hipError_t start(const ProductCall& p, const Choice& ch, int vec) {
+hipError_t start(const ProductCall& p, const Choice& ch) {
     typedef Shape<BF, AA, BA, WM, WN, MF> S;
     auto k = k_product<BF, AA, BA, WM, WN, MF>;
     if (S::kLds > 65536) {
@@ -319,17 +319,15 @@ hipError_t start(const ProductCall& p, const Choice& ch, int vec) {
     }
     hipLaunchKernelGGL(k, dim3((unsigned)(ch.tiles_m * ch.tiles_n * ch.splits)), dim3(S::T), S::kLds, p.stream, static_cast<const char*>(p.a), p.a_ld,
                        static_cast<const char*>(p.b), p.b_ld, p.c, p.c_ld, p.M, p.N, p.K, ch.tiles_m, ch.tiles_n, ch.steps_each,
-                       ch.splits > 1 ? p.partial : nullptr, vec, epilogue_of(p.ep));
+                       ch.splits > 1 ? p.partial : nullptr, epilogue_of(p.ep));
     return hipGetLastError();
 }
 
 template <bool BF, int WM, int WN, int MF>
-hipError_t start_by_order(const ProductCall& p, const Choice& ch, int vec) {
-    if (p.a_along) return p.b_along ? start<BF, true, true, WM, WN, MF>(p, ch, vec) : start<BF, true, false, WM, WN, MF>(p, ch, vec);
-    return start<BF, false, false, WM, WN, MF>(p, ch, vec);
+hipError_t start_by_order(const ProductCall& p, const Choice& ch) {
+    if (p.a_along) return p.b_along ? start<BF, true, true, WM, WN, MF>(p, ch) : start<BF, true, false, WM, WN, MF>(p, ch);
+    return start<BF, false, false, WM, WN, MF>(p, ch);
 }
-
-bool vec_aligned(const void* p, int64_t ld, int64_t z) { return !p || (reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld * z % 16 == 0); }
 
 }  // namespace
 
@@ -346,18 +344,16 @@ int64_t product_partial_bytes(bool bf16, int64_t M, int64_t N, int64_t K) {
 
 psgd_status launch_product(const ProductCall& p, std::string* what) {
     const Choice ch = choose(p.bf16, p.M, p.N, p.K);
-    const int64_t z = p.bf16 ? 2 : 4;
     if (ch.tiles_m * ch.tiles_n * ch.splits > 0x7fffffffLL) return PSGD_EUNSUPPORTED;
-    const int vec = vec_aligned(p.c, p.c_ld, z) && vec_aligned(p.ep.pre, p.ep.pre_ld, z) && vec_aligned(p.ep.residual, p.ep.residual_ld, z);
     hipError_t e;
-    if (!p.bf16) e = start_by_order<false, 2, 2, 4>(p, ch, vec);
-    else if (ch.big) e = start_by_order<true, 2, 4, 8>(p, ch, vec);
-    else e = start_by_order<true, 2, 2, 4>(p, ch, vec);
+    if (!p.bf16) e = start_by_order<false, 2, 2, 4>(p, ch);
+    else if (ch.big) e = start_by_order<true, 2, 4, 8>(p, ch);
+    else e = start_by_order<true, 2, 2, 4>(p, ch);
     if (e != hipSuccess) { *what = std::string("launch k_product: ") + hipGetErrorString(e); return PSGD_EHIP; }
     if (ch.splits > 1) {
         const int64_t blocks = (p.M * ((p.N + 7) / 8) + kBlock - 1) / kBlock;
         auto k = p.bf16 ? k_join<true> : k_join<false>;
-        hipLaunchKernelGGL(k, dim3((unsigned)blocks), dim3(kBlock), 0, p.stream, p.partial, ch.splits, p.c, p.c_ld, p.M, p.N, vec, epilogue_of(p.ep));
+        hipLaunchKernelGGL(k, dim3((unsigned)blocks), dim3(kBlock), 0, p.stream, p.partial, ch.splits, p.c, p.c_ld, p.M, p.N, epilogue_of(p.ep));
         e = hipGetLastError();
         if (e != hipSuccess) { *what = std::string("launch k_join: ") + hipGetErrorString(e); return PSGD_EHIP; }
     }
