@@ -2,6 +2,8 @@
 #ifndef PSGD_EPILOGUE_H
 #define PSGD_EPILOGUE_H
 
+#include <type_traits>
+
 #include "psgd_device.h"
 #include "psgd_product.h"
 #include "psgd_random.h"
@@ -16,21 +18,35 @@ __device__ __forceinline__ void st_any(void* p, int64_t at, float v, bool bf) {
     else static_cast<float*>(p)[at] = v;
 }
 
+// The hardware's exponential and reciprocal (one unit in the last place each) in place of the library's division and erff:
+// behind 4096 x 8192 x 2048 bf16 products gelu took 36 us on top of 123 with erff, silu 24 with a division, 256 vector-unit
+// lanes a CU being all there is for 65536 outputs a tile.
+constexpr float kLog2e = 1.4426950408889634f;
+
 // 1 / (1 + exp(-v)) and 1 minus that, both without cancellation or overflow
 __device__ __forceinline__ void logistic(float v, float& s, float& rest) {
-    const float e = __expf(-fabsf(v)), big = 1.f / (1.f + e), small = e * big;
+    const float e = __builtin_amdgcn_exp2f(-kLog2e * fabsf(v)), big = __builtin_amdgcn_rcpf(1.f + e), small = e * big;
     s = v >= 0.f ? big : small;
     rest = v >= 0.f ? small : big;
 }
 constexpr float kGeluA = 1.5957691216057308f, kGeluB = 0.044715f;   // 2 sqrt(2 / pi)
 
+// The normal distribution's tail beyond |z| and exp(-z^2 / 2): erfc by Abramowitz and Stegun 7.1.26 (error below 1.5e-7)
+__device__ __forceinline__ void normal_tail(float z, float& tail, float& e) {
+    const float x = fabsf(z) * 0.70710678118654752f, t = __builtin_amdgcn_rcpf(fmaf(0.3275911f, x, 1.f));
+    e = __builtin_amdgcn_exp2f(-kLog2e * x * x);
+    const float p = fmaf(fmaf(fmaf(fmaf(1.061405429f, t, -1.453152027f), t, 1.421413741f), t, -0.284496736f), t, 0.254829592f);
+    tail = 0.5f * p * t * e;
+}
+constexpr float kFar = 40.f;   // beyond this the tail is zero, also times an infinity
+
 __device__ __forceinline__ float act_of(float z, int act) {
-    float s, rest;
+    float tail, e;
     switch (act) {
         case PSGD_ACT_RELU: return z < 0.f ? 0.f : z;
-        case PSGD_ACT_GELU: return 0.5f * z * (1.f + erff(z * 0.70710678118654752f));
-        case PSGD_ACT_GELU_TANH: logistic(kGeluA * (z + kGeluB * z * z * z), s, rest); return z * s;   // (1 + tanh u) / 2
-        case PSGD_ACT_SILU: logistic(z, s, rest); return z * s;
+        case PSGD_ACT_GELU: normal_tail(z, tail, e); return (z < 0.f ? 0.f : z) - fminf(fabsf(z), kFar) * tail;
+        case PSGD_ACT_GELU_TANH: return z * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-kLog2e * kGeluA * z * fmaf(kGeluB * z, z, 1.f)));
+        case PSGD_ACT_SILU: return z * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-kLog2e * z));
         default: return z;
     }
 }
@@ -38,12 +54,44 @@ __device__ __forceinline__ float act_slope(float z, int act) {
     float s, rest;
     switch (act) {
         case PSGD_ACT_RELU: return z > 0.f ? 1.f : 0.f;
-        case PSGD_ACT_GELU: return 0.5f * (1.f + erff(z * 0.70710678118654752f)) + z * __expf(-0.5f * z * z) * 0.39894228040143268f;
+        case PSGD_ACT_GELU: {
+            float tail, e;
+            normal_tail(z, tail, e);
+            return (z >= 0.f ? 1.f - tail : tail) + fminf(fmaxf(z, -kFar), kFar) * e * 0.39894228040143268f;
+        }
         case PSGD_ACT_GELU_TANH:
             logistic(kGeluA * (z + kGeluB * z * z * z), s, rest);
             return s + z * s * rest * kGeluA * (1.f + 3.f * kGeluB * z * z);
         case PSGD_ACT_SILU: logistic(z, s, rest); return s * (1.f + z * rest);
         default: return 1.f;
+    }
+}
+
+// Eight at a time, the choice made once
+__device__ __forceinline__ void act_oct(float (&v)[8], int act) {
+    auto all = [&](auto kind) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = act_of(v[e], decltype(kind)::value);
+    };
+    switch (act) {
+        case PSGD_ACT_RELU: all(std::integral_constant<int, PSGD_ACT_RELU>()); break;
+        case PSGD_ACT_GELU: all(std::integral_constant<int, PSGD_ACT_GELU>()); break;
+        case PSGD_ACT_GELU_TANH: all(std::integral_constant<int, PSGD_ACT_GELU_TANH>()); break;
+        case PSGD_ACT_SILU: all(std::integral_constant<int, PSGD_ACT_SILU>()); break;
+        default: break;
+    }
+}
+__device__ __forceinline__ void slope_oct(const float (&z)[8], float (&v)[8], int act) {   // v times the slope at z
+    auto all = [&](auto kind) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] *= act_slope(z[e], decltype(kind)::value);
+    };
+    switch (act) {
+        case PSGD_ACT_RELU: all(std::integral_constant<int, PSGD_ACT_RELU>()); break;
+        case PSGD_ACT_GELU: all(std::integral_constant<int, PSGD_ACT_GELU>()); break;
+        case PSGD_ACT_GELU_TANH: all(std::integral_constant<int, PSGD_ACT_GELU_TANH>()); break;
+        case PSGD_ACT_SILU: all(std::integral_constant<int, PSGD_ACT_SILU>()); break;
+        default: break;
     }
 }
 
@@ -117,18 +165,16 @@ __device__ __forceinline__ void bias_oct(const Epilogue& ep, int64_t j, int64_t 
     for (int e = 0; e < 8; ++e) b[e] = ep.bias && j + e < N ? ld_any(ep.bias, j + e, ep.bias_bf) : 0.f;
 }
 
-// Columns j .. j + 7 (j a multiple of eight) of row i from their sums: one call of the generator.
+// Columns j .. j + 7 (j a multiple of eight, `count` of them exist) of row i from their sums: one call of the generator.
+// c_at, pre_at, residual_at: where they are in each array.
 template <bool BF>
-__device__ __forceinline__ void finish_oct(const Epilogue& ep, const Draw& d, void* c, int64_t c_ld, int64_t i, int64_t j, int64_t N,
-                                           const float (&sum)[8], const float (&bias)[8]) {
-    const int count = N - j < 8 ? (int)(N - j) : 8;
+__device__ __forceinline__ void finish_oct(const Epilogue& ep, const Draw& d, void* c, int64_t c_at, int64_t pre_at, int64_t residual_at,
+                                           int64_t i, int64_t j, int count, const float (&sum)[8], const float (&bias)[8]) {
     float v[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = sum[e] * ep.scale + bias[e];
-    if (ep.pre) st_oct<BF>(ep.pre, i * ep.pre_ld + j, count, v);
-    if (ep.act != PSGD_ACT_IDENTITY)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = act_of(v[e], ep.act);
+    if (ep.pre) st_oct<BF>(ep.pre, pre_at, count, v);
+    act_oct(v, ep.act);
     if (ep.drop.below) {
         const Words r = philox(d, (unsigned)(j >> 3), (unsigned)i);
 #pragma unroll
@@ -136,11 +182,11 @@ __device__ __forceinline__ void finish_oct(const Epilogue& ep, const Draw& d, vo
     }
     if (ep.residual) {
         float x[8];
-        ld_oct<BF>(ep.residual, i * ep.residual_ld + j, count, x);
+        ld_oct<BF>(ep.residual, residual_at, count, x);
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] += x[e];
     }
-    st_oct<BF>(c, i * c_ld + j, count, v);
+    st_oct<BF>(c, c_at, count, v);
 }
 
 }  // namespace psgd

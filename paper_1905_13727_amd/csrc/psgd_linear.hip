@@ -47,8 +47,7 @@ __global__ __launch_bounds__(kBlock) void k_dz(const void* dy, int64_t dy_ld, co
             if (act != PSGD_ACT_IDENTITY) {
                 float z[8];
                 ld_oct<BF>(pre, t * pre_ld + c0, count, z);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) v[j] *= act_slope(z[j], act);
+                slope_oct(z, v, act);
             }
             if (drop.below) {
                 const Words r = philox(d, (unsigned)(c0 >> 3), (unsigned)t);

@@ -1,19 +1,20 @@
 // Products of the linear layer on the matrix cores: C[i][j] = sum_l A(i, l) B(j, l).  x W^T has both operands along the
 // contraction, dz W the second across it, dz^T x both.
 //
-// A workgroup owns a tile of BM x BN outputs and goes along the contraction in steps of 128 bytes a row (64 bf16, 32 fp32), two
-// steps in LDS at a time: while the waves read one, the next is loaded straight into LDS, sixteen bytes a lane.
+// A workgroup owns a tile of BM x BN outputs and goes along the contraction in steps of 128 bytes a row (64 bf16, 32 fp32; with 64
+// bytes, half of a cache line a request, the large tile reached 1050 TFLOP/s instead of 1420), two steps in LDS at a time:
+// while one is read and multiplied, the next is loaded straight into LDS, sixteen bytes a lane.
 // Such a load writes 64 consecutive chunks of sixteen bytes, so which chunk of the operand lies where is decided by
 // which one a lane asks for; the places are permuted so that the reads of a wave meet no bank twice:
-//   along    row r holds its eight chunks in the order c ^ key(r), key the three bits in which the eight rows that are
-//            read together differ;
+//   along    chunk c of row r lies at place c ^ (r & 7) of its eight;
 //   across   row l of the contraction holds its chunks in the order c ^ f(l), f such that the four rows of a transposing read
 //            (ds_read_b64_tr_b16: four rows of the contraction, sixteen of the output) lie in different banks.
-// The sums go through LDS once more, 64 rows a wave at a time: a lane then holds eight consecutive columns of a row, one
+// The sums go through LDS once more, 32 rows a wave at a time: a lane then holds eight consecutive columns of a row, one
 // store of sixteen bytes (bf16) and one call of the generator.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "psgd_epilogue.h"
 
@@ -24,8 +25,6 @@ typedef short v4s __attribute__((ext_vector_type(4)));
 typedef short v8s __attribute__((ext_vector_type(8)));
 typedef __attribute__((address_space(3))) char lds_char;
 
-constexpr int kLanded = 0x0f70;   // vmcnt(0): loads to LDS count there; the other counters are left alone
-
 // ---- one operand of a tile ------------------------------------------------------------------------------------------
 
 // ROWS: outputs of the tile in this operand's dimension; Z: bytes an element; THREADS of the workgroup
@@ -33,36 +32,38 @@ template <int ROWS, int Z, bool ALONG, int THREADS>
 struct Operand {
     static constexpr int kElems = 16 / Z;                 // a chunk
     static constexpr int kStep = 128 / Z;                 // contraction of a step
-    static constexpr int kRowChunks = ALONG ? 8 : ROWS / kElems;
+    static constexpr int kRowChunks = ROWS / kElems;      // across: chunks of a row of the contraction
     static constexpr int kBytes = ROWS * 128;
     static constexpr int kLoads = kBytes / 16 / THREADS;
     static_assert(kBytes % (16 * THREADS) == 0, "whole loads");
 
-    static __device__ __forceinline__ int key(int line) {
-        if constexpr (ALONG) return line & 7;
-        else if constexpr (Z == 2) return ((line & 3) << 1) | (line & 8);
-        else return 0;
+    static __device__ __forceinline__ int key(int l) { return Z == 2 ? ((l & 3) << 1) | (l & 8) : 0; }   // across
+    // the row (along) or row of the contraction (across) and the chunk of it that this lane's i-th load brings
+    static __device__ __forceinline__ void place(int i, int& line, int& chunk) {
+        const int q = i * THREADS + threadIdx.x;
+        if constexpr (ALONG) {
+            line = q >> 3;
+            chunk = (q & 7) ^ (line & 7);
+        } else {
+            line = q / kRowChunks;
+            chunk = (q % kRowChunks) ^ key(line);
+        }
     }
     // byte offsets of this lane's chunks from the operand's base for the first step.  Outputs past the end are clamped to the last
     // ones: what they give is not stored.
     static __device__ __forceinline__ void sources(unsigned (&off)[kLoads], int64_t ld, int64_t extent) {
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
-            const int q = i * THREADS + threadIdx.x, line = q / kRowChunks, c = (q % kRowChunks) ^ key(line);
+            int line, c;
+            place(i, line, c);
             if constexpr (ALONG) {
                 const int row = line < extent ? line : (int)extent - 1;
-                off[i] = (unsigned)(row * ld * Z + c * 16);
+                off[i] = (unsigned)(row * (int)ld * Z + c * 16);
             } else {
                 const int last = ((int)(extent < ROWS ? extent : ROWS) + kElems - 1) / kElems - 1;
-                off[i] = (unsigned)(line * ld * Z + (c < last ? c : last) * 16);
+                off[i] = (unsigned)(line * (int)ld * Z + (c < last ? c : last) * 16);
             }
         }
-    }
-    // whether chunk i of a step with `left` elements of the contraction to go exists
-    static __device__ __forceinline__ bool inside(int i, int left) {
-        const int q = i * THREADS + threadIdx.x, line = q / kRowChunks;
-        if constexpr (ALONG) return ((q % kRowChunks) ^ key(line)) * kElems < left;
-        else return line < left;
     }
     static __device__ __forceinline__ void load(const char* base, const unsigned (&off)[kLoads], lds_char* to) {
         const buf_rsrc r = make_rsrc(base, 0x7fffffff);
@@ -71,42 +72,36 @@ struct Operand {
         for (int i = 0; i < kLoads; ++i)
             __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)(at + i * THREADS * 16), 16, (int)off[i], 0, 0, 0);
     }
-    // the last step, cut short: chunks past the end of the contraction are zero
+    // the last step, cut short: chunks past the end of the contraction, `left` elements on, are zero
     static __device__ __forceinline__ void load_cut(const char* base, const unsigned (&off)[kLoads], lds_char* to, int left) {
         const buf_rsrc r = make_rsrc(base, 0x7fffffff);
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
+            int line, c;
+            place(i, line, c);
             v4u t = v4u{0, 0, 0, 0};
-            if (inside(i, left)) t = __builtin_amdgcn_raw_buffer_load_b128(r, (int)off[i], 0, 0);
+            if ((ALONG ? c * kElems : line) < left) t = __builtin_amdgcn_raw_buffer_load_b128(r, (int)off[i], 0, 0);
             *reinterpret_cast<__attribute__((address_space(3))) v4u*>(to + (i * THREADS + threadIdx.x) * 16) = t;
         }
     }
     static __device__ __forceinline__ int64_t step_bytes(int64_t ld) { return ALONG ? 128 : kStep * ld * Z; }
 
-    // ---- fragments of half `h` (0, 1) of a step: lane i of lane group g reads output 16 f + i.  bf16: its eight of 32
-    static __device__ __forceinline__ v8bf frag16(const lds_char* s, int first, int f, int h) {
+    // Fragment f of half h of a step: lane i of lane group g holds output first + 16 f + i.  bf16: elements 8 g .. 8 g + 7 of the
+    // half's 32; fp32: 4 g .. 4 g + 3 of its 16
+    static __device__ __forceinline__ auto frag(const lds_char* s, int first, int f, int h) {
         const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
         if constexpr (ALONG) {
+            typedef typename std::conditional<Z == 2, v8bf, v4f>::type Frag;
             const int row = first + 16 * f + i;
-            const int c = (4 * h + g) ^ key(row);
-            return *reinterpret_cast<const __attribute__((address_space(3))) v8bf*>(s + row * 128 + c * 16);
-        } else {
-            // the four lines l .. l + 3 of a lane group's eight, sixteen outputs each: lane i asks for line i / 4, outputs 4 (i % 4)
+            return *reinterpret_cast<const __attribute__((address_space(3))) Frag*>(s + row * 128 + (((4 * h + g) ^ (row & 7)) << 4));
+        } else if constexpr (Z == 2) {
+            // the four rows l .. l + 3 of a lane group's eight, sixteen outputs each: lane i asks for row i / 4, outputs 4 (i % 4)
             const int l = 32 * h + 8 * g + (i >> 2), m = first + 16 * f + 4 * (i & 3);
             const lds_char* p = s + l * (ROWS * Z) + ((((m * Z) >> 4) ^ key(l)) << 4) + ((m * Z) & 15);
             typedef __attribute__((address_space(3))) v4s* lds_v4s;
             const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s)p);
             const v4s hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s)(p + 4 * (ROWS * Z)));   // key(l + 4) = key(l)
-            const v8s both = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-            return __builtin_bit_cast(v8bf, both);
-        }
-    }
-    // sixteen of the contraction, four to a lane: element e of lane group g is number 16 h + 4 g + e
-    static __device__ __forceinline__ v4f frag32(const lds_char* s, int first, int f, int h) {
-        const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
-        if constexpr (ALONG) {
-            const int row = first + 16 * f + i;
-            return *reinterpret_cast<const __attribute__((address_space(3))) v4f*>(s + row * 128 + (((4 * h + g) ^ key(row)) << 4));
+            return __builtin_bit_cast(v8bf, (v8s)__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
         } else {
             v4f t;
 #pragma unroll
@@ -137,9 +132,15 @@ struct Shape {   // WM x WN waves, each MF x 4 fragments of 16 x 16
     static constexpr int Z = BF ? 2 : 4;
     typedef Operand<BM, Z, AA, T> A;
     typedef Operand<BN, Z, BA, T> B;
-    static constexpr int kLds = 2 * (A::kBytes + B::kBytes);
-    static_assert(kLds >= WM * WN * 64 * 64 * 4 && MF % 4 == 0, "64 rows of sums a wave");
+    typedef typename std::conditional<BF, v8bf, v4f>::type Frag;
+    static constexpr int kStepBytes = A::kBytes + B::kBytes;
+    static constexpr int kLds = 2 * kStepBytes;
+    static constexpr int kPartBytes = 32 * 64 * 4;
+    static_assert(kLds >= WM * WN * kPartBytes && MF % 2 == 0, "32 rows of sums a wave");
 };
+
+// s_waitcnt: no load (to LDS too) in flight and every LDS access done
+constexpr int kLandedAndRead = 0x0070;
 
 // grid: tiles_m * tiles_n * splits.  With several splits of the contraction the sums go to `partial`, [split][M][N].
 template <bool BF, bool AA, bool BA, int WM, int WN, int MF>
@@ -149,16 +150,17 @@ __global__ __launch_bounds__(WM* WN* kWave, 2) void k_product(const char* a, int
     typedef Shape<BF, AA, BA, WM, WN, MF> S;
     typedef typename S::A A;
     typedef typename S::B B;
+    typedef typename S::Frag Frag;
     extern __shared__ __attribute__((aligned(16))) char lds_raw[];
     lds_char* const lds = (lds_char*)lds_raw;
-    constexpr int kBuf = A::kBytes + B::kBytes;
     int64_t tm, tn;
     const int64_t tiles = tiles_m * tiles_n, split = blockIdx.x / tiles;
     tile_of(blockIdx.x - split * tiles, tiles, tiles_m, tiles_n, tm, tn);
     const int64_t i0 = tm * S::BM, j0 = tn * S::BN;
-    const int64_t all = (K + A::kStep - 1) / A::kStep, s0 = split * steps_each, s1 = s0 + steps_each < all ? s0 + steps_each : all;
-    const bool cut = s1 == all && K % A::kStep != 0;   // the last step of this split ends inside
-    const int64_t whole = s1 - cut;
+    const int64_t all = (K + A::kStep - 1) / A::kStep, s0 = split * steps_each;
+    const int steps = (int)(s0 + steps_each < all ? steps_each : all - s0);
+    const int cut = s0 + steps == all ? (int)(K % A::kStep) : 0;   // what the last step holds, if it is cut short
+    const int whole = steps - (cut ? 1 : 0);
 
     unsigned a_off[A::kLoads], b_off[B::kLoads];
     A::sources(a_off, a_ld, M - i0);
@@ -173,64 +175,73 @@ __global__ __launch_bounds__(WM* WN* kWave, 2) void k_product(const char* a, int
 #pragma unroll
         for (int n = 0; n < 4; ++n) acc[m][n] = v4f{0.f, 0.f, 0.f, 0.f};
 
-    auto fetch = [&](int64_t s, int buf) {   // step s to LDS
-        lds_char* to = lds + buf * kBuf;
-        if (s < whole) {
-            A::load(ap, a_off, to);
-            B::load(bp, b_off, to + A::kBytes);
-        } else {
-            const int left = (int)(K - s * A::kStep);
-            A::load_cut(ap, a_off, to, left);
-            B::load_cut(bp, b_off, to + A::kBytes, left);
-        }
+    auto fetch = [&](int buf) {   // the next step to LDS
+        lds_char* to = lds + buf * S::kStepBytes;
+        A::load(ap, a_off, to);
+        B::load(bp, b_off, to + A::kBytes);
         ap += A::step_bytes(a_ld);
         bp += B::step_bytes(b_ld);
     };
-    auto multiply = [&](int buf) {
-        const lds_char *as = lds + buf * kBuf, *bs = as + A::kBytes;
+    auto fetch_cut = [&](int buf) {
+        lds_char* to = lds + buf * S::kStepBytes;
+        A::load_cut(ap, a_off, to, cut);
+        B::load_cut(bp, b_off, to + A::kBytes, cut);
+    };
+    auto read = [&](int buf, int h, Frag (&x)[MF], Frag (&y)[4]) {
+        const lds_char *as = lds + buf * S::kStepBytes, *bs = as + A::kBytes;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            if constexpr (BF) {
-                v8bf x[MF], y[4];
+        for (int n = 0; n < 4; ++n) y[n] = B::frag(bs, wn * 64, n, h);
 #pragma unroll
-                for (int n = 0; n < 4; ++n) y[n] = B::frag16(bs, wn * 64, n, h);
+        for (int m = 0; m < MF; ++m) x[m] = A::frag(as, wm * MF * 16, m, h);
+    };
+    auto multiply = [&](const Frag (&x)[MF], const Frag (&y)[4]) {
+        if constexpr (BF) {
 #pragma unroll
-                for (int m = 0; m < MF; ++m) x[m] = A::frag16(as, wm * MF * 16, m, h);
+            for (int m = 0; m < MF; ++m)
+#pragma unroll
+                for (int n = 0; n < 4; ++n) acc[m][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(y[n], x[m], acc[m][n], 0, 0, 0);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
 #pragma unroll
                 for (int m = 0; m < MF; ++m)
 #pragma unroll
-                    for (int n = 0; n < 4; ++n) acc[m][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(y[n], x[m], acc[m][n], 0, 0, 0);
-            } else {
-                v4f x[MF], y[4];
-#pragma unroll
-                for (int n = 0; n < 4; ++n) y[n] = B::frag32(bs, wn * 64, n, h);
-#pragma unroll
-                for (int m = 0; m < MF; ++m) x[m] = A::frag32(as, wm * MF * 16, m, h);
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-#pragma unroll
-                    for (int m = 0; m < MF; ++m)
-#pragma unroll
-                        for (int n = 0; n < 4; ++n) acc[m][n] = __builtin_amdgcn_mfma_f32_16x16x4f32(y[n][e], x[m][e], acc[m][n], 0, 0, 0);
-            }
+                    for (int n = 0; n < 4; ++n) acc[m][n] = __builtin_amdgcn_mfma_f32_16x16x4f32(y[n][e], x[m][e], acc[m][n], 0, 0, 0);
         }
     };
-
-    if (s0 < s1) {
-        fetch(s0, 0);
+    // The fragments of one half step are read while the other half's are multiplied, across the steps too: the barrier that
+    // hands a buffer over stands in the middle of a step, where a half's products are ready to issue on both sides of it.
+    if (steps > 0) {
+        Frag x0[MF], y0[4], x1[MF], y1[4];
+        if (whole > 0) fetch(0);
+        else fetch_cut(0);
+        __builtin_amdgcn_s_waitcnt(kLandedAndRead);
+        __syncthreads();
+        if (whole > 1) fetch(1);
+        else if (steps > 1) fetch_cut(1);
+        read(0, 0, x0, y0);
         int buf = 0;
-        for (int64_t s = s0; s < s1; ++s, buf ^= 1) {
-            __builtin_amdgcn_s_waitcnt(kLanded);
-            __syncthreads();   // this step's loads have landed, the other half is read
-            if (s + 1 < s1) fetch(s + 1, buf ^ 1);
-            multiply(buf);
+        for (int s = 0; s < steps; ++s, buf ^= 1) {
+            read(buf, 1, x1, y1);
+            __builtin_amdgcn_sched_barrier(0);
+            multiply(x0, y0);
+            __builtin_amdgcn_sched_barrier(0);
+            if (s + 1 < steps) {
+                __builtin_amdgcn_s_waitcnt(kLandedAndRead);   // step s + 1 has landed, this step's fragments are in registers
+                __syncthreads();
+                if (s + 2 < whole) fetch(buf);
+                else if (s + 2 < steps) fetch_cut(buf);
+                read(buf ^ 1, 0, x0, y0);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            multiply(x1, y1);
         }
     }
 
-    // 64 x 64 sums of a wave: row r holds its sixteen quads in the order q ^ (r & 15)
+    // 32 x 64 sums of a wave at a time: row r holds its sixteen quads in the order q ^ (r & 15)
     __syncthreads();
     const int lane = threadIdx.x & 63, g = lane >> 4;
-    lds_char* const mine = lds + wave * 16384;
+    lds_char* const mine = lds + wave * S::kPartBytes;
     const int64_t j = j0 + wn * 64 + 8 * (lane & 7);
     Draw d{};
     float bias[8] = {};
@@ -238,28 +249,40 @@ __global__ __launch_bounds__(WM* WN* kWave, 2) void k_product(const char* a, int
         if (ep.drop.below) d = make_draw(ep.drop.rng, ep.drop.offset);
         bias_oct(ep, j, N, bias);
     }
-#pragma unroll
-    for (int part = 0; part < MF / 4; ++part) {
-#pragma unroll
-        for (int m = 0; m < 4; ++m)
-#pragma unroll
-            for (int n = 0; n < 4; ++n)
-                *reinterpret_cast<__attribute__((address_space(3))) v4f*>(mine + (16 * m + (lane & 15)) * 256 + (((4 * n + g) ^ (lane & 15)) << 4)) =
-                    acc[4 * part + m][n];
-        const int64_t i1 = i0 + wm * MF * 16 + 64 * part;
+    const int count = N - j < 8 ? (int)(N - j) : 8;
+    const int64_t first = i0 + wm * MF * 16 + (lane >> 3);
+    const int rows = (int)(M - first < MF * 16 ? M - first : MF * 16);   // this lane's rows of the wave's, from `first` on
+    int64_t c_at = first * c_ld + j, pre_at = first * ep.pre_ld + j, residual_at = first * ep.residual_ld + j, i = first;
+    if (partial) c_at = (split * M + first) * N + j, c_ld = N;
 #pragma unroll 1
-        for (int r = lane >> 3; r < 64; r += 8) {
-            const int64_t i = i1 + r;
-            if (i >= M || j >= N) break;
-            float sum[8];
+    for (int part = 0; part < MF / 2; ++part) {
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const v4f t = *reinterpret_cast<const __attribute__((address_space(3))) v4f*>(mine + r * 256 + (((2 * (lane & 7) + h) ^ (r & 15)) << 4));
+        for (int q = 0; q < MF / 2; ++q)
+            if (q == part)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) sum[4 * h + e] = t[e];
+                for (int m = 0; m < 2; ++m)
+#pragma unroll
+                    for (int n = 0; n < 4; ++n)
+                        *reinterpret_cast<__attribute__((address_space(3))) v4f*>(mine + (16 * m + (lane & 15)) * 256 + (((4 * n + g) ^ (lane & 15)) << 4)) =
+                            acc[2 * q + m][n];
+        const lds_char* from = mine + (lane >> 3) * 256;
+#pragma unroll 2
+        for (int r = 0; r < 32; r += 8) {
+            if (32 * part + r < rows && count > 0) {
+                float sum[8];
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const v4f t = *reinterpret_cast<const __attribute__((address_space(3))) v4f*>(from + r * 256 + (((2 * (lane & 7) + h) ^ (((lane >> 3) + r) & 15)) << 4));
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) sum[4 * h + e] = t[e];
+                }
+                if (partial) st_oct<false>(partial, c_at, count, sum);
+                else finish_oct<BF>(ep, d, c, c_at, pre_at, residual_at, i, j, count, sum, bias);
             }
-            if (partial) st_oct<false>(partial, (split * M + i) * N + j, N - j < 8 ? (int)(N - j) : 8, sum);
-            else finish_oct<BF>(ep, d, c, c_ld, i, j, N, sum, bias);
+            i += 8;
+            c_at += 8 * c_ld;
+            pre_at += 8 * ep.pre_ld;
+            residual_at += 8 * ep.residual_ld;
         }
     }
 }
@@ -282,7 +305,7 @@ __global__ __launch_bounds__(kBlock) void k_join(const float* partial, int64_t s
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] += x[e];
     }
-    finish_oct<BF>(ep, d, c, c_ld, i, j, N, v, bias);
+    finish_oct<BF>(ep, d, c, i * c_ld + j, i * ep.pre_ld + j, i * ep.residual_ld + j, i, j, count, v, bias);
 }
 
 namespace {
