@@ -9,18 +9,16 @@
 
 namespace psgd {
 
-// dst [rows][dst_ld] = src [rows][cols], rounded if dst is bf16 and src is not; columns up to dst_ld are zero.
+// bf16 dst [rows][dst_ld] = src [rows][cols], rounded if src is fp32; dst_ld a multiple of eight, columns from `cols` on are zero.
 // One lane: eight columns.
-template <bool SBF, bool DBF>
-__global__ __launch_bounds__(kBlock) void k_lay_out(const void* src, int64_t src_ld, void* dst, int64_t dst_ld, int64_t rows, int64_t cols) {
-    const int64_t per_row = (dst_ld + 7) / 8, at = (int64_t)blockIdx.x * kBlock + threadIdx.x;
+template <bool SBF>
+__global__ __launch_bounds__(kBlock) void k_lay_out(const void* src, int64_t src_ld, bf16_t* dst, int64_t dst_ld, int64_t rows, int64_t cols) {
+    const int64_t per_row = dst_ld / 8, at = (int64_t)blockIdx.x * kBlock + threadIdx.x;
     if (at >= rows * per_row) return;
     const int64_t row = at / per_row, j = 8 * (at - row * per_row);
     float x[8];
-    const int count = cols - j < 8 ? (int)(cols - j) : 8;
-    ld_oct<SBF>(src, row * src_ld + j, count, x);
-    const int to = dst_ld - j < 8 ? (int)(dst_ld - j) : 8;
-    st_oct<DBF>(dst, row * dst_ld + j, to, x);
+    ld_oct<SBF>(src, row * src_ld + j, cols - j < 8 ? (int)(cols - j) : 8, x);
+    st_oct<true>(dst, row * dst_ld + j, 8, x);
 }
 
 // dz = D(dy) act'(pre) without the factor of the elements that stay, which goes into the products' epilogues: where the
@@ -104,62 +102,61 @@ bool failed(const char* name, std::string* what) {
     return true;
 }
 
-bool vec_aligned(const void* p, int64_t ld, int64_t z) { return !p || (reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld * z % 16 == 0); }
+bool vec_aligned(const void* p, int64_t ld) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld % 8 == 0; }   // bf16
 
 // Where the parts of the workspace are
 struct Parts {
-    int64_t w, x, dz, db, partial, bytes;   // offsets; w = -1: the weights are read where they are
-    int64_t k_ld, n_ld;                     // row lengths of laid-out operands
+    int64_t w, x, dz, db, partial;   // offsets; w = -1: the weights are read where they are
+    int64_t k_ld, n_ld;              // row lengths of laid-out operands
 };
 
 Parts parts_of(const LinearCall& c) {
     Parts p{};
-    const int64_t z = c.bf16 ? 2 : 4, run = 16 / z;
-    if (c.T == 0) return p;
-    p.k_ld = up(c.k, run);
-    p.n_ld = up(c.n, run);
+    const int64_t z = c.bf16 ? 2 : 4;
+    p.k_ld = c.bf16 ? up(c.k, 8) : c.k;
+    p.n_ld = c.bf16 ? up(c.n, 8) : c.n;
     int64_t at = 0;
     auto take = [&](int64_t bytes) { const int64_t was = at; at += up(bytes, 256); return was; };
-    p.w = c.param_bf16 != c.bf16 || c.k % run ? take(c.n * p.k_ld * z) : -1;
-    p.x = take(c.T * p.k_ld * z);
+    p.w = c.bf16 && (!c.param_bf16 || c.k % 8) ? take(c.n * p.k_ld * z) : -1;
+    p.x = c.bf16 ? take(c.T * p.k_ld * z) : 0;
     p.dz = take(c.T * p.n_ld * z);
     p.db = take(up(c.T, kDzRows) / kDzRows * c.n * 4);
-    p.partial = take(std::max({product_partial_bytes(c.bf16, c.T, c.n, c.k), product_partial_bytes(c.bf16, c.T, c.k, c.n),
-                               product_partial_bytes(c.bf16, c.n, c.k, c.T)}));
-    p.bytes = at;
+    p.partial = at;
     return p;
 }
 
-bool lay_out(const void* src, int64_t src_ld, bool src_bf, void* dst, int64_t dst_ld, bool dst_bf, int64_t rows, int64_t cols, hipStream_t s,
-             std::string* what) {
-    const int64_t blocks = (rows * ((dst_ld + 7) / 8) + kBlock - 1) / kBlock;
-    auto k = src_bf ? k_lay_out<true, true> : dst_bf ? k_lay_out<false, true> : k_lay_out<false, false>;
-    hipLaunchKernelGGL(k, dim3((unsigned)blocks), dim3(kBlock), 0, s, src, src_ld, dst, dst_ld, rows, cols);
+bool lay_out(const void* src, int64_t src_ld, bool src_bf, void* dst, int64_t dst_ld, int64_t rows, int64_t cols, hipStream_t s, std::string* what) {
+    const int64_t blocks = (rows * (dst_ld / 8) + kBlock - 1) / kBlock;
+    auto k = src_bf ? k_lay_out<true> : k_lay_out<false>;
+    hipLaunchKernelGGL(k, dim3((unsigned)blocks), dim3(kBlock), 0, s, src, src_ld, static_cast<bf16_t*>(dst), dst_ld, rows, cols);
     return !failed("k_lay_out", what);
 }
 
-// The weights or the input as an operand of a product: in place if rows and base allow, else laid out
+// The weights or the input as an operand of a product: in place if it can read them there, else laid out
 bool weights(const LinearCall& c, const Parts& p, const void** w, int64_t* ld, std::string* what) {
     *w = c.w;
     *ld = c.k;
     if (p.w < 0) return true;
     *w = static_cast<char*>(c.workspace) + p.w;
     *ld = p.k_ld;
-    return lay_out(c.w, c.k, c.param_bf16, const_cast<void*>(*w), *ld, c.bf16, c.n, c.k, static_cast<hipStream_t>(c.stream), what);
+    return lay_out(c.w, c.k, c.param_bf16, const_cast<void*>(*w), *ld, c.n, c.k, static_cast<hipStream_t>(c.stream), what);
 }
 bool input(const LinearCall& c, const Parts& p, const void** x, int64_t* ld, std::string* what) {
     *x = c.x;
     *ld = c.x_ld;
-    const int64_t z = c.bf16 ? 2 : 4;
-    if (vec_aligned(c.x, c.x_ld, z) && c.k * z % 16 == 0) return true;
+    if (!c.bf16 || (vec_aligned(c.x, c.x_ld) && c.k % 8 == 0)) return true;
     *x = static_cast<char*>(c.workspace) + p.x;
     *ld = p.k_ld;
-    return lay_out(c.x, c.x_ld, c.bf16, const_cast<void*>(*x), *ld, c.bf16, c.T, c.k, static_cast<hipStream_t>(c.stream), what);
+    return lay_out(c.x, c.x_ld, true, const_cast<void*>(*x), *ld, c.T, c.k, static_cast<hipStream_t>(c.stream), what);
 }
 
 }  // namespace
 
-int64_t linear_workspace_bytes(const LinearCall& c) { return parts_of(c).bytes; }
+int64_t linear_workspace_bytes(const LinearCall& c) {
+    if (c.T == 0) return 0;
+    return parts_of(c).partial + std::max({product_partial_bytes(c.bf16, c.T, c.n, c.k), product_partial_bytes(c.bf16, c.T, c.k, c.n),
+                                           product_partial_bytes(c.bf16, c.n, c.k, c.T)});
+}
 
 psgd_status launch_linear_forward(const LinearCall& c, std::string* what) {
     const Parts p = parts_of(c);
@@ -188,7 +185,6 @@ psgd_status launch_linear_forward(const LinearCall& c, std::string* what) {
 psgd_status launch_linear_backward(const LinearCall& c, std::string* what) {
     const hipStream_t s = static_cast<hipStream_t>(c.stream);
     const Parts p = parts_of(c);
-    const int64_t z = c.bf16 ? 2 : 4;
     const float scale = c.drop.below ? c.drop.factor : 1.f;
     if (c.T == 0 && c.accumulate) return PSGD_OK;
     char* const ws = static_cast<char*>(c.workspace);
@@ -196,7 +192,7 @@ psgd_status launch_linear_backward(const LinearCall& c, std::string* what) {
     const void* dz = c.dy;
     int64_t dz_ld = c.dy_ld;
     if (c.T > 0) {
-        const bool direct = c.act == PSGD_ACT_IDENTITY && !c.drop.below && vec_aligned(c.dy, c.dy_ld, z) && c.n * z % 16 == 0;
+        const bool direct = c.act == PSGD_ACT_IDENTITY && !c.drop.below && (!c.bf16 || (vec_aligned(c.dy, c.dy_ld) && c.n % 8 == 0));
         if (!direct) {
             dz = ws + p.dz;
             dz_ld = p.n_ld;

@@ -86,7 +86,7 @@ psgd_status psgd_linear_forward(psgd_plan* plan, const psgd_linear* op, const vo
     const size_t z = c.bf16 ? 2 : 4;
     if (!x || !y || !aligned(x, z) || !aligned(y, z) || !aligned(residual, z) || !aligned(pre, z) || !aligned(param, 16))
         return PSGD_EINVAL;
-    if (psgd::linear_workspace_bytes(c) > 0 && (!workspace || !aligned(workspace, 256))) return PSGD_EINVAL;
+    if (!workspace || !aligned(workspace, 256)) return PSGD_EINVAL;
     c.w = at(param, plan->tensor_flat_off[op->weight], c.param_bf16);
     c.bias = op->bias >= 0 ? at(param, plan->tensor_flat_off[op->bias], c.param_bf16) : nullptr;
     c.x = x;
@@ -117,7 +117,7 @@ psgd_status psgd_linear_backward(psgd_plan* plan, const psgd_linear* op, const v
         if (c.act != PSGD_ACT_IDENTITY && (!pre || !aligned(pre, z))) return PSGD_EINVAL;
         if (dx && (!param || !aligned(param, 16))) return PSGD_EINVAL;
         if (grad && (!x || !aligned(x, z))) return PSGD_EINVAL;
-        if (psgd::linear_workspace_bytes(c) > 0 && (!workspace || !aligned(workspace, 256))) return PSGD_EINVAL;
+        if (!workspace || !aligned(workspace, 256)) return PSGD_EINVAL;
     }
     c.w = param ? at(param, plan->tensor_flat_off[op->weight], c.param_bf16) : nullptr;
     c.x = x;
@@ -150,6 +150,7 @@ static psgd_status dropout(psgd_dtype dtype, int64_t rows, int64_t cols, const v
         return PSGD_EINVAL;
     for (int64_t v : {rows, cols, c.x_ld, c.residual_ld, c.y_ld})
         if (v > 0x7fffffffLL) return PSGD_EUNSUPPORTED;
+    if (rows > 0 && cols > (int64_t(1) << 42) / rows) return PSGD_EUNSUPPORTED;
     if (rows == 0 || cols == 0) return PSGD_OK;
     c.bf16 = dtype == PSGD_BF16;
     const size_t z = c.bf16 ? 2 : 4;

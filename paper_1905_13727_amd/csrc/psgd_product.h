@@ -24,9 +24,9 @@ struct EpilogueHost {
     DropHost drop{};
 };
 
-// Either operand lies along the contraction (`along`: element (i, l) at i * ld + l) or across it (l * ld + i).  Bases are aligned
-// to 16 bytes, ld is a multiple of 16 bytes, and so is the contiguous extent, or what follows it up to the next multiple is
-// readable and zero.
+// Either operand lies along the contraction (`along`: element (i, l) at i * ld + l) or across it (l * ld + i).  bf16: bases are
+// aligned to 16 bytes, ld is a multiple of 16 bytes, and so is the contiguous extent, or what follows it up to the next multiple
+// is readable and zero.  fp32: anything.
 struct ProductCall {
     bool bf16;
     const void* a;
@@ -43,7 +43,7 @@ struct ProductCall {
     hipStream_t stream;
 };
 
-// Scratch for the product and for any with fewer rows M
+// Scratch for the product and for any with fewer rows M or a shorter contraction
 int64_t product_partial_bytes(bool bf16, int64_t M, int64_t N, int64_t K);
 psgd_status launch_product(const ProductCall& c, std::string* what);
 

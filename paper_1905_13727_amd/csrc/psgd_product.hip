@@ -9,6 +9,8 @@
 //   along    chunk c of row r lies at place c ^ (r & 7) of its eight;
 //   across   row l of the contraction holds its chunks in the order c ^ f(l), f such that the four rows of a transposing read
 //            (ds_read_b64_tr_b16: four rows of the contraction, sixteen of the output) lie in different banks.
+// fp32 operands are loaded through registers instead: the fp32 matrix instructions leave time enough, and a row may then begin
+// at any element.
 // The sums go through LDS once more, 32 rows a wave at a time: a lane then holds eight consecutive columns of a row, one
 // store of sixteen bytes (bf16) and one call of the generator.
 #include <hip/hip_runtime.h>
@@ -37,7 +39,7 @@ struct Operand {
     static constexpr int kLoads = kBytes / 16 / THREADS;
     static_assert(kBytes % (16 * THREADS) == 0, "whole loads");
 
-    static __device__ __forceinline__ int key(int l) { return Z == 2 ? ((l & 3) << 1) | (l & 8) : 0; }   // across
+    static __device__ __forceinline__ int key(int l) { return Z == 2 ? ((l & 3) << 1) | (kRowChunks > 8 ? l & 8 : 0) : 0; }   // across
     // the row (along) or row of the contraction (across) and the chunk of it that this lane's i-th load brings
     static __device__ __forceinline__ void place(int i, int& line, int& chunk) {
         const int q = i * THREADS + threadIdx.x;
@@ -65,12 +67,38 @@ struct Operand {
             }
         }
     }
+    // straight to LDS
     static __device__ __forceinline__ void load(const char* base, const unsigned (&off)[kLoads], lds_char* to) {
         const buf_rsrc r = make_rsrc(base, 0x7fffffff);
         lds_char* at = to + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave) * (kWave * 16);
 #pragma unroll
         for (int i = 0; i < kLoads; ++i)
             __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)(at + i * THREADS * 16), 16, (int)off[i], 0, 0, 0);
+    }
+    // to registers, and from there.  `end`: where the operand's memory ends (what lies behind reads as zero); `left`: elements of
+    // the contraction to go, those past the end are zero.
+    static __device__ __forceinline__ void load(const char* base, const unsigned (&off)[kLoads], const char* end, int64_t left, v4u (&held)[kLoads]) {
+        const int64_t room = end - base;
+        const buf_rsrc r = make_rsrc(base, room < 0x7fffffff ? room : 0x7fffffff);
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            int line, c;
+            place(i, line, c);
+            held[i] = __builtin_amdgcn_raw_buffer_load_b128(r, !ALONG && line >= left ? (int)kOutOfRange : (int)off[i], 0, 0);
+        }
+    }
+    static __device__ __forceinline__ void store(v4u (&held)[kLoads], int64_t left, lds_char* to) {
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            if (ALONG && left < kStep) {
+                int line, c;
+                place(i, line, c);
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if ((c * 16 + e * 4) / Z >= left) held[i][e] = 0;
+            }
+            *reinterpret_cast<__attribute__((address_space(3))) v4u*>(to + (i * THREADS + threadIdx.x) * 16) = held[i];
+        }
     }
     // the last step, cut short: chunks past the end of the contraction, `left` elements on, are zero
     static __device__ __forceinline__ void load_cut(const char* base, const unsigned (&off)[kLoads], lds_char* to, int left) {
@@ -126,28 +154,28 @@ __device__ __forceinline__ void tile_of(int64_t number, int64_t count, int64_t t
     tn = t / high;
 }
 
-template <bool BF, bool AA, bool BA, int WM, int WN, int MF>
-struct Shape {   // WM x WN waves, each MF x 4 fragments of 16 x 16
-    static constexpr int BM = WM * MF * 16, BN = WN * 64, T = WM * WN * kWave;
+template <bool BF, bool AA, bool BA, int WM, int WN, int MF, int NF>
+struct Shape {   // WM x WN waves, each MF x NF fragments of 16 x 16
+    static constexpr int BM = WM * MF * 16, BN = WN * NF * 16, T = WM * WN * kWave;
     static constexpr int Z = BF ? 2 : 4;
     typedef Operand<BM, Z, AA, T> A;
     typedef Operand<BN, Z, BA, T> B;
     typedef typename std::conditional<BF, v8bf, v4f>::type Frag;
     static constexpr int kStepBytes = A::kBytes + B::kBytes;
     static constexpr int kLds = 2 * kStepBytes;
-    static constexpr int kPartBytes = 32 * 64 * 4;
-    static_assert(kLds >= WM * WN * kPartBytes && MF % 2 == 0, "32 rows of sums a wave");
+    static constexpr int kPartBytes = 32 * NF * 64;   // 32 rows of a wave's sums
+    static_assert(kLds >= WM * WN * kPartBytes && MF % 2 == 0 && (NF == 4 || NF == 2), "32 rows of sums a wave");
 };
 
 // s_waitcnt: no load (to LDS too) in flight and every LDS access done
 constexpr int kLandedAndRead = 0x0070;
 
 // grid: tiles_m * tiles_n * splits.  With several splits of the contraction the sums go to `partial`, [split][M][N].
-template <bool BF, bool AA, bool BA, int WM, int WN, int MF>
+template <bool BF, bool AA, bool BA, int WM, int WN, int MF, int NF>
 __global__ __launch_bounds__(WM* WN* kWave, 2) void k_product(const char* a, int64_t a_ld, const char* b, int64_t b_ld, void* c, int64_t c_ld,
                                                              int64_t M, int64_t N, int64_t K, int64_t tiles_m, int64_t tiles_n,
                                                              int64_t steps_each, float* partial, Epilogue ep) {
-    typedef Shape<BF, AA, BA, WM, WN, MF> S;
+    typedef Shape<BF, AA, BA, WM, WN, MF, NF> S;
     typedef typename S::A A;
     typedef typename S::B B;
     typedef typename S::Frag Frag;
@@ -169,56 +197,73 @@ __global__ __launch_bounds__(WM* WN* kWave, 2) void k_product(const char* a, int
     const char* bp = b + (BA ? j0 * b_ld : j0) * S::Z + s0 * B::step_bytes(b_ld);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), wm = wave / WN, wn = wave % WN;
 
-    v4f acc[MF][4];
+    v4f acc[MF][NF];
 #pragma unroll
     for (int m = 0; m < MF; ++m)
 #pragma unroll
-        for (int n = 0; n < 4; ++n) acc[m][n] = v4f{0.f, 0.f, 0.f, 0.f};
+        for (int n = 0; n < NF; ++n) acc[m][n] = v4f{0.f, 0.f, 0.f, 0.f};
 
-    auto fetch = [&](int buf) {   // the next step to LDS
+    // bf16: step s goes to LDS at once; fp32: to registers, and by settle() to LDS one barrier later
+    const char* const a_end = a + (AA ? (M - 1) * a_ld + K : (K - 1) * a_ld + M) * S::Z;
+    const char* const b_end = b + (BA ? (N - 1) * b_ld + K : (K - 1) * b_ld + N) * S::Z;
+    v4u a_held[BF ? 1 : A::kLoads], b_held[BF ? 1 : B::kLoads];
+    auto fetch = [&](int s, int buf) {
         lds_char* to = lds + buf * S::kStepBytes;
-        A::load(ap, a_off, to);
-        B::load(bp, b_off, to + A::kBytes);
+        if constexpr (BF) {
+            if (s < whole) {
+                A::load(ap, a_off, to);
+                B::load(bp, b_off, to + A::kBytes);
+            } else {
+                A::load_cut(ap, a_off, to, cut);
+                B::load_cut(bp, b_off, to + A::kBytes, cut);
+            }
+        } else {
+            const int64_t left = s < whole ? A::kStep : cut;
+            A::load(ap, a_off, a_end, left, a_held);
+            B::load(bp, b_off, b_end, left, b_held);
+        }
         ap += A::step_bytes(a_ld);
         bp += B::step_bytes(b_ld);
     };
-    auto fetch_cut = [&](int buf) {
-        lds_char* to = lds + buf * S::kStepBytes;
-        A::load_cut(ap, a_off, to, cut);
-        B::load_cut(bp, b_off, to + A::kBytes, cut);
+    auto settle = [&](int s, int buf) {
+        if constexpr (!BF) {
+            lds_char* to = lds + buf * S::kStepBytes;
+            const int64_t left = s < whole ? A::kStep : cut;
+            A::store(a_held, left, to);
+            B::store(b_held, left, to + A::kBytes);
+        }
+        __builtin_amdgcn_s_waitcnt(kLandedAndRead);
     };
-    auto read = [&](int buf, int h, Frag (&x)[MF], Frag (&y)[4]) {
+    auto read = [&](int buf, int h, Frag (&x)[MF], Frag (&y)[NF]) {
         const lds_char *as = lds + buf * S::kStepBytes, *bs = as + A::kBytes;
 #pragma unroll
-        for (int n = 0; n < 4; ++n) y[n] = B::frag(bs, wn * 64, n, h);
+        for (int n = 0; n < NF; ++n) y[n] = B::frag(bs, wn * NF * 16, n, h);
 #pragma unroll
         for (int m = 0; m < MF; ++m) x[m] = A::frag(as, wm * MF * 16, m, h);
     };
-    auto multiply = [&](const Frag (&x)[MF], const Frag (&y)[4]) {
+    auto multiply = [&](const Frag (&x)[MF], const Frag (&y)[NF]) {
         if constexpr (BF) {
 #pragma unroll
             for (int m = 0; m < MF; ++m)
 #pragma unroll
-                for (int n = 0; n < 4; ++n) acc[m][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(y[n], x[m], acc[m][n], 0, 0, 0);
+                for (int n = 0; n < NF; ++n) acc[m][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(y[n], x[m], acc[m][n], 0, 0, 0);
         } else {
 #pragma unroll
             for (int e = 0; e < 4; ++e)
 #pragma unroll
                 for (int m = 0; m < MF; ++m)
 #pragma unroll
-                    for (int n = 0; n < 4; ++n) acc[m][n] = __builtin_amdgcn_mfma_f32_16x16x4f32(y[n][e], x[m][e], acc[m][n], 0, 0, 0);
+                    for (int n = 0; n < NF; ++n) acc[m][n] = __builtin_amdgcn_mfma_f32_16x16x4f32(y[n][e], x[m][e], acc[m][n], 0, 0, 0);
         }
     };
     // The fragments of one half step are read while the other half's are multiplied, across the steps too: the barrier that
     // hands a buffer over stands in the middle of a step, where a half's products are ready to issue on both sides of it.
     if (steps > 0) {
-        Frag x0[MF], y0[4], x1[MF], y1[4];
-        if (whole > 0) fetch(0);
-        else fetch_cut(0);
-        __builtin_amdgcn_s_waitcnt(kLandedAndRead);
+        Frag x0[MF], y0[NF], x1[MF], y1[NF];
+        fetch(0, 0);
+        settle(0, 0);
         __syncthreads();
-        if (whole > 1) fetch(1);
-        else if (steps > 1) fetch_cut(1);
+        if (steps > 1) fetch(1, 1);
         read(0, 0, x0, y0);
         int buf = 0;
         for (int s = 0; s < steps; ++s, buf ^= 1) {
@@ -227,10 +272,9 @@ __global__ __launch_bounds__(WM* WN* kWave, 2) void k_product(const char* a, int
             multiply(x0, y0);
             __builtin_amdgcn_sched_barrier(0);
             if (s + 1 < steps) {
-                __builtin_amdgcn_s_waitcnt(kLandedAndRead);   // step s + 1 has landed, this step's fragments are in registers
+                settle(s + 1, buf ^ 1);   // step s + 1 has landed, this step's fragments are in registers
                 __syncthreads();
-                if (s + 2 < whole) fetch(buf);
-                else if (s + 2 < steps) fetch_cut(buf);
+                if (s + 2 < steps) fetch(s + 2, buf);
                 read(buf ^ 1, 0, x0, y0);
             }
             __builtin_amdgcn_sched_barrier(0);
@@ -238,11 +282,12 @@ __global__ __launch_bounds__(WM* WN* kWave, 2) void k_product(const char* a, int
         }
     }
 
-    // 32 x 64 sums of a wave at a time: row r holds its sixteen quads in the order q ^ (r & 15)
+    // 32 rows of a wave's sums at a time: row r holds its quads in the order q ^ (r & (4 NF - 1))
     __syncthreads();
-    const int lane = threadIdx.x & 63, g = lane >> 4;
+    constexpr int kQuads = 4 * NF, kAcross = 2 * NF, kRowsAtOnce = 64 / kAcross;   // quads of a row, lanes along one, rows of all lanes
+    const int lane = threadIdx.x & 63, g = lane >> 4, lr = lane / kAcross, lc = lane % kAcross;
     lds_char* const mine = lds + wave * S::kPartBytes;
-    const int64_t j = j0 + wn * 64 + 8 * (lane & 7);
+    const int64_t j = j0 + wn * NF * 16 + 8 * lc;
     Draw d{};
     float bias[8] = {};
     if (!partial) {
@@ -250,7 +295,7 @@ __global__ __launch_bounds__(WM* WN* kWave, 2) void k_product(const char* a, int
         bias_oct(ep, j, N, bias);
     }
     const int count = N - j < 8 ? (int)(N - j) : 8;
-    const int64_t first = i0 + wm * MF * 16 + (lane >> 3);
+    const int64_t first = i0 + wm * MF * 16 + lr;
     const int rows = (int)(M - first < MF * 16 ? M - first : MF * 16);   // this lane's rows of the wave's, from `first` on
     int64_t c_at = first * c_ld + j, pre_at = first * ep.pre_ld + j, residual_at = first * ep.residual_ld + j, i = first;
     if (partial) c_at = (split * M + first) * N + j, c_ld = N;
@@ -262,27 +307,28 @@ __global__ __launch_bounds__(WM* WN* kWave, 2) void k_product(const char* a, int
 #pragma unroll
                 for (int m = 0; m < 2; ++m)
 #pragma unroll
-                    for (int n = 0; n < 4; ++n)
-                        *reinterpret_cast<__attribute__((address_space(3))) v4f*>(mine + (16 * m + (lane & 15)) * 256 + (((4 * n + g) ^ (lane & 15)) << 4)) =
-                            acc[2 * q + m][n];
-        const lds_char* from = mine + (lane >> 3) * 256;
+                    for (int n = 0; n < NF; ++n) {
+                        const int r = 16 * m + (lane & 15);
+                        *reinterpret_cast<__attribute__((address_space(3))) v4f*>(mine + (r * kQuads + ((4 * n + g) ^ (r & (kQuads - 1)))) * 16) = acc[2 * q + m][n];
+                    }
 #pragma unroll 2
-        for (int r = 0; r < 32; r += 8) {
-            if (32 * part + r < rows && count > 0) {
+        for (int r0 = 0; r0 < 32; r0 += kRowsAtOnce) {
+            if (32 * part + r0 < rows && count > 0) {
+                const int r = r0 + lr;
                 float sum[8];
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    const v4f t = *reinterpret_cast<const __attribute__((address_space(3))) v4f*>(from + r * 256 + (((2 * (lane & 7) + h) ^ (((lane >> 3) + r) & 15)) << 4));
+                    const v4f t = *reinterpret_cast<const __attribute__((address_space(3))) v4f*>(mine + (r * kQuads + ((2 * lc + h) ^ (r & (kQuads - 1)))) * 16);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) sum[4 * h + e] = t[e];
                 }
                 if (partial) st_oct<false>(partial, c_at, count, sum);
                 else finish_oct<BF>(ep, d, c, c_at, pre_at, residual_at, i, j, count, sum, bias);
             }
-            i += 8;
-            c_at += 8 * c_ld;
-            pre_at += 8 * ep.pre_ld;
-            residual_at += 8 * ep.residual_ld;
+            i += kRowsAtOnce;
+            c_at += kRowsAtOnce * c_ld;
+            pre_at += kRowsAtOnce * ep.pre_ld;
+            residual_at += kRowsAtOnce * ep.residual_ld;
         }
     }
 }
@@ -312,30 +358,49 @@ namespace {
 
 constexpr int kCUs = 256;
 
+// A split takes four steps at least, and there are no more tiles and splits than the units hold at a time, so that the sums
+// take at most 64 MiB whatever the sizes.
+constexpr int64_t kMostSplits = 32, kLeastSteps = 4, kMostPartial = int64_t(kCUs) * 256 * 256 * 4;
+constexpr int64_t most_parts(int side) { return kCUs * (side == 64 ? 4 : side == 128 ? 2 : 1); }
+static_assert(most_parts(64) * 64 * 64 * 4 <= kMostPartial && most_parts(128) * 128 * 128 * 4 <= kMostPartial, "fits");
+
 struct Choice {
-    bool big;          // tiles of 256 x 256 (bf16), else 128 x 128
+    int side;          // tiles of side x side
     int64_t splits, steps_each, tiles_m, tiles_n;
 };
 
+// The tile and the division of the contraction with the least expected time: steps of a tile one after the other, as many tiles
+// at a time as there are compute units, and the sums of the splits written and read again.
 Choice choose(bool bf16, int64_t M, int64_t N, int64_t K) {
-    Choice c{};
     const int64_t steps = (K + (bf16 ? 63 : 31)) / (bf16 ? 64 : 32);
-    const int64_t t256 = ((M + 255) / 256) * ((N + 255) / 256);
-    c.big = bf16 && t256 >= kCUs;
-    const int64_t side = c.big ? 256 : 128;
-    c.tiles_m = (M + side - 1) / side;
-    c.tiles_n = (N + side - 1) / side;
-    const int64_t tiles = c.tiles_m * c.tiles_n;
-    c.splits = std::max<int64_t>(1, std::min<int64_t>(kCUs / std::max<int64_t>(tiles, 1), steps / 8));
-    c.steps_each = std::max<int64_t>(1, (steps + c.splits - 1) / c.splits);
-    c.splits = std::max<int64_t>(1, (steps + c.steps_each - 1) / c.steps_each);
-    return c;
+    Choice best{};
+    double least = 0;
+    for (int side : {256, 128, 64}) {
+        if (side == 256 && !bf16) continue;
+        const int64_t tm = (M + side - 1) / side, tn = (N + side - 1) / side, tiles = tm * tn;
+        // us a step with the unit full, and at the least, of one tile by itself
+        const double full = bf16 ? (side == 256 ? 1.46 : side == 128 ? 0.47 : 0.17) : (side == 128 ? 1.8 : 0.48);
+        const double alone = bf16 ? (side == 256 ? 1.46 : side == 128 ? 0.7 : 0.5) : (side == 128 ? 2.0 : 0.8);
+        const double ends = side == 256 ? 10 : side == 128 ? 5 : 3;   // first loads, epilogue
+        for (int64_t splits = 1; splits <= kMostSplits && (splits == 1 || (splits <= steps / kLeastSteps && tiles * splits <= most_parts(side))); ++splits) {
+            const int64_t each = std::max<int64_t>(1, (steps + splits - 1) / splits), parts = std::max<int64_t>(1, (steps + each - 1) / each);
+            if (parts != splits) continue;
+            const double rounds = (double)((tiles * splits + kCUs - 1) / kCUs);
+            double us = each * std::max(alone, rounds * full) + ends * std::max(1.0, side == 256 ? rounds : rounds / 2);
+            if (splits > 1) us += 4 + 2e-6 * 4 * splits * M * N / 4;
+            if (best.side == 0 || us < least) {
+                least = us;
+                best = Choice{side, splits, each, tm, tn};
+            }
+        }
+    }
+    return best;
 }
 
-template <bool BF, bool AA, bool BA, int WM, int WN, int MF>
+template <bool BF, bool AA, bool BA, int WM, int WN, int MF, int NF>
 hipError_t start(const ProductCall& p, const Choice& ch) {
-    typedef Shape<BF, AA, BA, WM, WN, MF> S;
-    auto k = k_product<BF, AA, BA, WM, WN, MF>;
+    typedef Shape<BF, AA, BA, WM, WN, MF, NF> S;
+    auto k = k_product<BF, AA, BA, WM, WN, MF, NF>;
     if (S::kLds > 65536) {
         const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(k), hipFuncAttributeMaxDynamicSharedMemorySize, S::kLds);
         if (e != hipSuccess) return e;
@@ -346,32 +411,26 @@ hipError_t start(const ProductCall& p, const Choice& ch) {
     return hipGetLastError();
 }
 
-template <bool BF, int WM, int WN, int MF>
+template <bool BF, int WM, int WN, int MF, int NF>
 hipError_t start_by_order(const ProductCall& p, const Choice& ch) {
-    if (p.a_along) return p.b_along ? start<BF, true, true, WM, WN, MF>(p, ch) : start<BF, true, false, WM, WN, MF>(p, ch);
-    return start<BF, false, false, WM, WN, MF>(p, ch);
+    if (p.a_along) return p.b_along ? start<BF, true, true, WM, WN, MF, NF>(p, ch) : start<BF, true, false, WM, WN, MF, NF>(p, ch);
+    return start<BF, false, false, WM, WN, MF, NF>(p, ch);
 }
 
 }  // namespace
 
 int64_t product_partial_bytes(bool bf16, int64_t M, int64_t N, int64_t K) {
-    // the most of any smaller M too (a program sizes its workspace once, for its longest batch)
-    int64_t most = 0;
-    for (int64_t m = std::min<int64_t>(M, 128);; m = std::min<int64_t>(M, m + 128)) {
-        const Choice ch = choose(bf16, m, N, K);
-        if (ch.splits > 1) most = std::max(most, ch.splits * m * N * 4);
-        if (m >= M || m / 128 >= kCUs) break;
-    }
-    return most;
+    const int64_t splits = std::min<int64_t>(kMostSplits, (K + (bf16 ? 63 : 31)) / (bf16 ? 64 : 32) / kLeastSteps);
+    return splits > 1 ? std::min(splits * M * N * 4, kMostPartial) : 0;
 }
 
 psgd_status launch_product(const ProductCall& p, std::string* what) {
     const Choice ch = choose(p.bf16, p.M, p.N, p.K);
     if (ch.tiles_m * ch.tiles_n * ch.splits > 0x7fffffffLL) return PSGD_EUNSUPPORTED;
     hipError_t e;
-    if (!p.bf16) e = start_by_order<false, 2, 2, 4>(p, ch);
-    else if (ch.big) e = start_by_order<true, 2, 4, 8>(p, ch);
-    else e = start_by_order<true, 2, 2, 4>(p, ch);
+    if (!p.bf16) e = ch.side == 128 ? start_by_order<false, 2, 2, 4, 4>(p, ch) : start_by_order<false, 2, 2, 2, 2>(p, ch);
+    else if (ch.side == 256) e = start_by_order<true, 2, 4, 8, 4>(p, ch);
+    else e = ch.side == 128 ? start_by_order<true, 2, 2, 4, 4>(p, ch) : start_by_order<true, 2, 2, 2, 2>(p, ch);
     if (e != hipSuccess) { *what = std::string("launch k_product: ") + hipGetErrorString(e); return PSGD_EHIP; }
     if (ch.splits > 1) {
         const int64_t blocks = (p.M * ((p.N + 7) / 8) + kBlock - 1) / kBlock;
