@@ -13,7 +13,8 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB_PATH = os.path.join(HERE, "libpsgd.so")
 SOURCES = ["psgd_plan.cpp", "psgd_kernels.hip", "psgd_resident.hip", "psgd_highrank.hip", "psgd_onesweep.hip", "psgd_sparse.hip",
-           "psgd_operators.cpp", "psgd_linear.hip", "psgd_product.hip", "psgd_dropout.hip"]
+           "psgd_operators.cpp", "psgd_linear.hip", "psgd_product.hip", "psgd_few_tokens.hip",
+           "psgd_dropout.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [

@@ -132,22 +132,40 @@ bool lay_out(const void* src, int64_t src_ld, bool src_bf, void* dst, int64_t ds
     return !failed("k_lay_out", what);
 }
 
-// The weights or the input as an operand of a product: in place if it can read them there, else laid out
-bool weights(const LinearCall& c, const Parts& p, const void** w, int64_t* ld, std::string* what) {
-    *w = c.w;
-    *ld = c.k;
-    if (p.w < 0) return true;
-    *w = static_cast<char*>(c.workspace) + p.w;
-    *ld = p.k_ld;
-    return lay_out(c.w, c.k, c.param_bf16, const_cast<void*>(*w), *ld, c.n, c.k, static_cast<hipStream_t>(c.stream), what);
+// Whether operands of a bf16 product that cannot go straight to LDS are laid out for it first: a pass over them against slower
+// loads in every tile.  us, laid out / in place: forward, fp32 weights of 8192 x 2048, 300 tokens 38 / 33, 700 49 / 49, 1500 72 / 85, 4000
+// 131 / 194; 4096 x 4095 bf16, both operands, 300 45 / 41, 700 58 / 66, 4000 133 / 201; 2600 x 650 bf16 1500 28 / 19, 4000 46 / 39; 50304 x
+// 2048 fp32 300 218 / 152, 1500 398 / 495.  The weight gradient, which reads the input alone in another place: 1000 x 1001, 4000 tokens
+// 36 / 37, 2600 x 650 1500 26 / 29, 700 17 / 16; 4096 x 4095 300 30 / 33.
+bool lay_out_pays(const LinearCall& c, bool weight_gradient) {
+    const double work = (double)c.T * (double)c.n * (double)c.k;
+    return weight_gradient ? work >= 2e9 : c.T >= 640 && work >= 6e9;
 }
-bool input(const LinearCall& c, const Parts& p, const void** x, int64_t* ld, std::string* what) {
+
+// The weights or the input as operand B or A of the product q.M x q.N x q.K
+bool weights(const LinearCall& c, const Parts& p, ProductCall& q, std::string* what) {
+    q.b = c.w;
+    q.b_ld = c.k;
+    q.b_fp32 = c.bf16 && !c.param_bf16;
+    q.b_ready = !q.b_fp32 && c.k % 8 == 0;
+    if (!c.bf16 || q.b_ready || !lay_out_pays(c, false)) return true;
+    void* to = static_cast<char*>(c.workspace) + p.w;
+    q.b = to;
+    q.b_ld = p.k_ld;
+    q.b_fp32 = false;
+    q.b_ready = true;
+    return lay_out(c.w, c.k, c.param_bf16, to, p.k_ld, c.n, c.k, q.stream, what);
+}
+bool input(const LinearCall& c, const Parts& p, const ProductCall& q, const void** x, int64_t* ld, bool* ready, std::string* what) {
     *x = c.x;
     *ld = c.x_ld;
-    if (!c.bf16 || (vec_aligned(c.x, c.x_ld) && c.k % 8 == 0)) return true;
-    *x = static_cast<char*>(c.workspace) + p.x;
+    *ready = vec_aligned(c.x, c.x_ld) && c.k % 8 == 0;
+    if (!c.bf16 || *ready || !lay_out_pays(c, !q.a_along)) return true;
+    void* to = static_cast<char*>(c.workspace) + p.x;
+    *x = to;
     *ld = p.k_ld;
-    return lay_out(c.x, c.x_ld, true, const_cast<void*>(*x), *ld, c.T, c.k, static_cast<hipStream_t>(c.stream), what);
+    *ready = true;
+    return lay_out(c.x, c.x_ld, true, to, p.k_ld, c.T, c.k, q.stream, what);
 }
 
 }  // namespace
@@ -159,26 +177,29 @@ int64_t linear_workspace_bytes(const LinearCall& c) {
 }
 
 psgd_status launch_linear_forward(const LinearCall& c, std::string* what) {
+    EpilogueHost ep;
+    ep.bias = c.bias;
+    ep.bias_bf = c.param_bf16;
+    ep.act = c.act;
+    ep.pre = c.pre;
+    ep.pre_ld = c.pre_ld;
+    ep.residual = c.residual;
+    ep.residual_ld = c.residual_ld;
+    ep.drop = c.drop;
+    if (few_tokens(c)) return launch_few_tokens(c, ep, what);
     const Parts p = parts_of(c);
     ProductCall q{};
     q.bf16 = c.bf16;
     q.a_along = q.b_along = true;
-    if (!weights(c, p, &q.b, &q.b_ld, what) || !input(c, p, &q.a, &q.a_ld, what)) return PSGD_EHIP;
     q.c = c.y;
     q.c_ld = c.y_ld;
     q.M = c.T;
     q.N = c.n;
     q.K = c.k;
-    q.ep.bias = c.bias;
-    q.ep.bias_bf = c.param_bf16;
-    q.ep.act = c.act;
-    q.ep.pre = c.pre;
-    q.ep.pre_ld = c.pre_ld;
-    q.ep.residual = c.residual;
-    q.ep.residual_ld = c.residual_ld;
-    q.ep.drop = c.drop;
+    q.ep = ep;
     q.partial = reinterpret_cast<float*>(static_cast<char*>(c.workspace) + p.partial);
     q.stream = static_cast<hipStream_t>(c.stream);
+    if (!weights(c, p, q, what) || !input(c, p, q, &q.a, &q.a_ld, &q.a_ready, what)) return PSGD_EHIP;
     return launch_product(q, what);
 }
 
@@ -191,12 +212,14 @@ psgd_status launch_linear_backward(const LinearCall& c, std::string* what) {
     const int64_t blocks = up(c.T, kDzRows) / kDzRows;
     const void* dz = c.dy;
     int64_t dz_ld = c.dy_ld;
+    bool dz_ready = false;
     if (c.T > 0) {
-        const bool direct = c.act == PSGD_ACT_IDENTITY && !c.drop.below && (!c.bf16 || (vec_aligned(c.dy, c.dy_ld) && c.n % 8 == 0));
-        if (!direct) {
+        const bool direct = c.act == PSGD_ACT_IDENTITY && !c.drop.below;
+        if (!direct) {   // rows padded with zeros to multiples of sixteen bytes
             dz = ws + p.dz;
             dz_ld = p.n_ld;
         }
+        dz_ready = !direct || (vec_aligned(c.dy, c.dy_ld) && c.n % 8 == 0);
         if (!direct || c.db) {
             auto k = c.bf16 ? k_dz<true> : k_dz<false>;
             if ((c.n + 255) / 256 * blocks > 0x7fffffffLL) return PSGD_EUNSUPPORTED;
@@ -218,26 +241,26 @@ psgd_status launch_linear_backward(const LinearCall& c, std::string* what) {
     q.stream = s;
     q.a = dz;
     q.a_ld = dz_ld;
+    q.a_ready = dz_ready;
     q.N = c.k;
     if (c.dx && c.T > 0) {
         q.a_along = true;
-        if (!weights(c, p, &q.b, &q.b_ld, what)) return PSGD_EHIP;
         q.c = c.dx;
         q.c_ld = c.dx_ld;
         q.M = c.T;
         q.K = c.n;
+        if (!weights(c, p, q, what)) return PSGD_EHIP;
         const psgd_status st = launch_product(q, what);
         if (st != PSGD_OK) return st;
     }
     if (c.dw) {
         q.a_along = false;
-        q.b = nullptr;
-        q.b_ld = 0;
-        if (c.T > 0 && !input(c, p, &q.b, &q.b_ld, what)) return PSGD_EHIP;
+        q.b_fp32 = false;
         q.c = c.dw;
         q.c_ld = c.k;
         q.M = c.n;
         q.K = c.T;
+        if (!input(c, p, q, &q.b, &q.b_ld, &q.b_ready, what)) return PSGD_EHIP;
         if (c.accumulate) {
             q.ep.residual = c.dw;
             q.ep.residual_ld = c.k;

@@ -24,17 +24,17 @@ struct EpilogueHost {
     DropHost drop{};
 };
 
-// Either operand lies along the contraction (`along`: element (i, l) at i * ld + l) or across it (l * ld + i).  bf16: bases are
-// aligned to 16 bytes, ld is a multiple of 16 bytes, and so is the contiguous extent, or what follows it up to the next multiple
-// is readable and zero.  fp32: anything.
+// Either operand lies along the contraction (`along`: element (i, l) at i * ld + l) or across it (l * ld + i).  bf16: `ready` says
+// that the base is aligned to 16 bytes, ld a multiple of eight, and so the contiguous extent, or that what follows it up to the next
+// multiple is readable and zero; with both ready the operands go straight to LDS.  b_fp32: B is fp32, and rounded.
 struct ProductCall {
     bool bf16;
     const void* a;
     int64_t a_ld;
-    bool a_along;
+    bool a_along, a_ready;
     const void* b;
     int64_t b_ld;
-    bool b_along;
+    bool b_along, b_ready, b_fp32;
     void* c;
     int64_t c_ld;
     int64_t M, N, K;
@@ -46,6 +46,11 @@ struct ProductCall {
 // Scratch for the product and for any with fewer rows M or a shorter contraction
 int64_t product_partial_bytes(bool bf16, int64_t M, int64_t N, int64_t K);
 psgd_status launch_product(const ProductCall& c, std::string* what);
+
+// The forward product of at most kFewTokens tokens, without scratch and whatever the operands' types and alignment
+constexpr int64_t kFewTokens = 32;
+bool few_tokens(const LinearCall& c);
+psgd_status launch_few_tokens(const LinearCall& c, const EpilogueHost& ep, std::string* what);
 
 }  // namespace psgd
 

@@ -9,8 +9,9 @@
 //   along    chunk c of row r lies at place c ^ (r & 7) of its eight;
 //   across   row l of the contraction holds its chunks in the order c ^ f(l), f such that the four rows of a transposing read
 //            (ds_read_b64_tr_b16: four rows of the contraction, sixteen of the output) lie in different banks.
-// fp32 operands are loaded through registers instead: the fp32 matrix instructions leave time enough, and a row may then begin
-// at any element.
+// Operands that cannot be loaded that way go through registers instead: fp32 ones (their matrix instructions leave time enough,
+// and a row may then begin at any element), bf16 ones whose rows do not begin on multiples of sixteen bytes, and fp32 weights
+// rounded to bf16 on the way.
 // The sums go through LDS once more, 32 rows a wave at a time: a lane then holds eight consecutive columns of a row, one
 // store of sixteen bytes (bf16) and one call of the generator.
 #include <hip/hip_runtime.h>
@@ -29,14 +30,19 @@ typedef __attribute__((address_space(3))) char lds_char;
 
 // ---- one operand of a tile ------------------------------------------------------------------------------------------
 
-// ROWS: outputs of the tile in this operand's dimension; Z: bytes an element; THREADS of the workgroup
-template <int ROWS, int Z, bool ALONG, int THREADS>
+enum Source { kStraight, kBf16, kFp32 };   // straight to LDS; through registers, from bf16 or fp32 in memory
+
+// ROWS: outputs of the tile in this operand's dimension; Z: bytes an element in LDS; THREADS of the workgroup
+template <int ROWS, int Z, bool ALONG, Source SRC, int THREADS>
 struct Operand {
-    static constexpr int kElems = 16 / Z;                 // a chunk
+    static_assert(Z == 2 || SRC == kFp32, "fp32 products read fp32");
+    static constexpr int kElems = 16 / Z;                 // a chunk in LDS
+    static constexpr int kSrc = SRC == kFp32 ? 4 : 2;     // bytes an element in memory
     static constexpr int kStep = 128 / Z;                 // contraction of a step
     static constexpr int kRowChunks = ROWS / kElems;      // across: chunks of a row of the contraction
     static constexpr int kBytes = ROWS * 128;
     static constexpr int kLoads = kBytes / 16 / THREADS;
+    static constexpr int kWords = Z == 2 && SRC == kFp32 ? 2 : 1;   // registers of four words a chunk
     static_assert(kBytes % (16 * THREADS) == 0, "whole loads");
 
     static __device__ __forceinline__ int key(int l) { return Z == 2 ? ((l & 3) << 1) | (kRowChunks > 8 ? l & 8 : 0) : 0; }   // across
@@ -60,10 +66,11 @@ struct Operand {
             place(i, line, c);
             if constexpr (ALONG) {
                 const int row = line < extent ? line : (int)extent - 1;
-                off[i] = (unsigned)(row * (int)ld * Z + c * 16);
+                off[i] = (unsigned)((row * (int)ld + c * kElems) * kSrc);
             } else {
-                const int last = ((int)(extent < ROWS ? extent : ROWS) + kElems - 1) / kElems - 1;
-                off[i] = (unsigned)(line * (int)ld * Z + (c < last ? c : last) * 16);
+                const int many = (int)(extent < ROWS ? extent : ROWS), last = (many + kElems - 1) / kElems - 1;
+                const int e = SRC == kBf16 ? (c * kElems < many - 8 ? c * kElems : many - 8) : (c < last ? c : last) * kElems;
+                off[i] = (unsigned)((line * (int)ld + e) * kSrc);
             }
         }
     }
@@ -75,29 +82,89 @@ struct Operand {
         for (int i = 0; i < kLoads; ++i)
             __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)(at + i * THREADS * 16), 16, (int)off[i], 0, 0, 0);
     }
-    // to registers, and from there.  `end`: where the operand's memory ends (what lies behind reads as zero); `left`: elements of
-    // the contraction to go, those past the end are zero.
-    static __device__ __forceinline__ void load(const char* base, const unsigned (&off)[kLoads], const char* end, int64_t left, v4u (&held)[kLoads]) {
-        const int64_t room = end - base;
-        const buf_rsrc r = make_rsrc(base, room < 0x7fffffff ? room : 0x7fffffff);
+    // To registers, and by store() to LDS.  `left`: elements of the contraction to go, those past the end are zero; `extent`: outputs
+    // from the tile's first on, those past the end are never stored, but memory may end there.
+    // bf16: a chunk that the row's end cuts (or that lies behind it) is read as the row's last eight elements and shifted into place by
+    // store(), so that no lane reads past the end and none reads element by element; `tiny` (a row of fewer than eight): it does.
+    static __device__ __forceinline__ void load(const char* base, const unsigned (&off)[kLoads], int64_t ld, int64_t extent, int64_t left,
+                                                bool tiny, v4u (&held)[kLoads * kWords]) {
+        if constexpr (SRC == kFp32) {   // what lies behind the end reads as zero
+            const int64_t room = (ALONG ? (extent - 1) * ld + left : (left - 1) * ld + extent) * 4;
+            const buf_rsrc r = make_rsrc(base, room < 0x7fffffff ? room : 0x7fffffff);
 #pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-            int line, c;
-            place(i, line, c);
-            held[i] = __builtin_amdgcn_raw_buffer_load_b128(r, !ALONG && line >= left ? (int)kOutOfRange : (int)off[i], 0, 0);
-        }
-    }
-    static __device__ __forceinline__ void store(v4u (&held)[kLoads], int64_t left, lds_char* to) {
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-            if (ALONG && left < kStep) {
+            for (int i = 0; i < kLoads; ++i) {
                 int line, c;
                 place(i, line, c);
+                const int at = !ALONG && line >= left ? (int)kOutOfRange : (int)off[i];
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if ((c * 16 + e * 4) / Z >= left) held[i][e] = 0;
+                for (int h = 0; h < kWords; ++h) held[i * kWords + h] = __builtin_amdgcn_raw_buffer_load_b128(r, at + 16 * h, 0, 0);
             }
-            *reinterpret_cast<__attribute__((address_space(3))) v4u*>(to + (i * THREADS + threadIdx.x) * 16) = held[i];
+        } else if (tiny) {
+            const int many = (int)(ALONG ? left : extent < ROWS ? extent : ROWS);
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) {
+                int line, c;
+                place(i, line, c);
+                const int count = !ALONG && line >= left ? 0 : many - c * kElems;
+                const int row = ALONG && line >= extent ? (int)extent - 1 : line;
+                v4u t = v4u{0, 0, 0, 0};
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (e < count) t[e >> 1] |= (unsigned)reinterpret_cast<const bf16_t*>(base)[row * (int)ld + c * kElems + e] << (16 * (e & 1));
+                held[i] = t;
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) {
+                int at = (int)off[i];
+                if (left < kStep) {
+                    int line, c;
+                    place(i, line, c);
+                    if constexpr (ALONG) at += c * kElems < (int)left - 8 ? 0 : ((int)left - 8 - c * kElems) * 2;
+                    else at -= line < left ? 0 : (line - (int)left + 1) * (int)ld * 2;
+                }
+                held[i] = *reinterpret_cast<const v4u_any*>(base + at);
+            }
+        }
+    }
+    static __device__ __forceinline__ void store(const v4u (&held)[kLoads * kWords], int64_t extent, int64_t left, bool tiny, lds_char* to) {
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            v4u t[kWords];
+#pragma unroll
+            for (int h = 0; h < kWords; ++h) t[h] = held[i * kWords + h];
+            if constexpr (SRC == kFp32) {
+                if (ALONG && left < kStep) {
+                    int line, c;
+                    place(i, line, c);
+#pragma unroll
+                    for (int h = 0; h < kWords; ++h)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (c * kElems + 4 * h + e >= left) t[h][e] = 0;
+                }
+            } else if (!tiny && ((!ALONG && extent < ROWS) || left < kStep)) {
+                int line, c;
+                place(i, line, c);
+                const int many = (int)(ALONG ? left : extent < ROWS ? extent : ROWS);
+                int count = many - c * kElems;
+                count = (!ALONG && line >= left) || count < 0 ? 0 : count > 8 ? 8 : count;
+                const int words = (8 - count) >> 1;   // the last `count` of eight elements become the first
+                v4u u = t[0];
+                u = words & 2 ? v4u{u[2], u[3], 0, 0} : u;
+                u = words & 1 ? v4u{u[1], u[2], u[3], 0} : u;
+                if (count & 1) u = v4u{u[0] >> 16 | u[1] << 16, u[1] >> 16 | u[2] << 16, u[2] >> 16 | u[3] << 16, u[3] >> 16};
+                t[0] = count == 0 ? v4u{0, 0, 0, 0} : u;
+            }
+            if constexpr (kWords == 2) {   // rounded to nearest even
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const v4f x = __builtin_bit_cast(v4f, t[h]);
+                    t[0][2 * h] = pack_bf16x2(x.x, x.y);
+                    t[0][2 * h + 1] = pack_bf16x2(x.z, x.w);
+                }
+            }
+            *reinterpret_cast<__attribute__((address_space(3))) v4u*>(to + (i * THREADS + threadIdx.x) * 16) = t[0];
         }
     }
     // the last step, cut short: chunks past the end of the contraction, `left` elements on, are zero
@@ -112,7 +179,7 @@ struct Operand {
             *reinterpret_cast<__attribute__((address_space(3))) v4u*>(to + (i * THREADS + threadIdx.x) * 16) = t;
         }
     }
-    static __device__ __forceinline__ int64_t step_bytes(int64_t ld) { return ALONG ? 128 : kStep * ld * Z; }
+    static __device__ __forceinline__ int64_t step_bytes(int64_t ld) { return (ALONG ? 1 : ld) * kStep * kSrc; }
 
     // Fragment f of half h of a step: lane i of lane group g holds output first + 16 f + i.  bf16: elements 8 g .. 8 g + 7 of the
     // half's 32; fp32: 4 g .. 4 g + 3 of its 16
@@ -154,12 +221,12 @@ __device__ __forceinline__ void tile_of(int64_t number, int64_t count, int64_t t
     tn = t / high;
 }
 
-template <bool BF, bool AA, bool BA, int WM, int WN, int MF, int NF>
+template <bool BF, bool AA, bool BA, Source AS, Source BS, int WM, int WN, int MF, int NF>
 struct Shape {   // WM x WN waves, each MF x NF fragments of 16 x 16
     static constexpr int BM = WM * MF * 16, BN = WN * NF * 16, T = WM * WN * kWave;
     static constexpr int Z = BF ? 2 : 4;
-    typedef Operand<BM, Z, AA, T> A;
-    typedef Operand<BN, Z, BA, T> B;
+    typedef Operand<BM, Z, AA, AS, T> A;
+    typedef Operand<BN, Z, BA, BS, T> B;
     typedef typename std::conditional<BF, v8bf, v4f>::type Frag;
     static constexpr int kStepBytes = A::kBytes + B::kBytes;
     static constexpr int kLds = 2 * kStepBytes;
@@ -171,11 +238,11 @@ struct Shape {   // WM x WN waves, each MF x NF fragments of 16 x 16
 constexpr int kLandedAndRead = 0x0070;
 
 // grid: tiles_m * tiles_n * splits.  With several splits of the contraction the sums go to `partial`, [split][M][N].
-template <bool BF, bool AA, bool BA, int WM, int WN, int MF, int NF>
+template <bool BF, bool AA, bool BA, Source AS, Source BS, int WM, int WN, int MF, int NF>
 __global__ __launch_bounds__(WM* WN* kWave, 2) void k_product(const char* a, int64_t a_ld, const char* b, int64_t b_ld, void* c, int64_t c_ld,
                                                              int64_t M, int64_t N, int64_t K, int64_t tiles_m, int64_t tiles_n,
                                                              int64_t steps_each, float* partial, Epilogue ep) {
-    typedef Shape<BF, AA, BA, WM, WN, MF, NF> S;
+    typedef Shape<BF, AA, BA, AS, BS, WM, WN, MF, NF> S;
     typedef typename S::A A;
     typedef typename S::B B;
     typedef typename S::Frag Frag;
@@ -193,8 +260,8 @@ __global__ __launch_bounds__(WM* WN* kWave, 2) void k_product(const char* a, int
     unsigned a_off[A::kLoads], b_off[B::kLoads];
     A::sources(a_off, a_ld, M - i0);
     B::sources(b_off, b_ld, N - j0);
-    const char* ap = a + (AA ? i0 * a_ld : i0) * S::Z + s0 * A::step_bytes(a_ld);
-    const char* bp = b + (BA ? j0 * b_ld : j0) * S::Z + s0 * B::step_bytes(b_ld);
+    const char* ap = a + (AA ? i0 * a_ld : i0) * A::kSrc + s0 * A::step_bytes(a_ld);
+    const char* bp = b + (BA ? j0 * b_ld : j0) * B::kSrc + s0 * B::step_bytes(b_ld);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), wm = wave / WN, wn = wave % WN;
 
     v4f acc[MF][NF];
@@ -203,35 +270,32 @@ __global__ __launch_bounds__(WM* WN* kWave, 2) void k_product(const char* a, int
 #pragma unroll
         for (int n = 0; n < NF; ++n) acc[m][n] = v4f{0.f, 0.f, 0.f, 0.f};
 
-    // bf16: step s goes to LDS at once; fp32: to registers, and by settle() to LDS one barrier later
-    const char* const a_end = a + (AA ? (M - 1) * a_ld + K : (K - 1) * a_ld + M) * S::Z;
-    const char* const b_end = b + (BA ? (N - 1) * b_ld + K : (K - 1) * b_ld + N) * S::Z;
-    v4u a_held[BF ? 1 : A::kLoads], b_held[BF ? 1 : B::kLoads];
+    // Step s: straight to LDS at once, through registers by settle() one barrier later.  `left` of the contraction from step s on,
+    // for the loads through registers.
+    v4u a_held[A::kLoads * A::kWords], b_held[B::kLoads * B::kWords];
     auto fetch = [&](int s, int buf) {
         lds_char* to = lds + buf * S::kStepBytes;
-        if constexpr (BF) {
-            if (s < whole) {
-                A::load(ap, a_off, to);
-                B::load(bp, b_off, to + A::kBytes);
-            } else {
-                A::load_cut(ap, a_off, to, cut);
-                B::load_cut(bp, b_off, to + A::kBytes, cut);
-            }
+        const int64_t left = K - (s0 + s) * A::kStep;
+        if constexpr (AS == kStraight) {
+            if (s < whole) A::load(ap, a_off, to);
+            else A::load_cut(ap, a_off, to, cut);
         } else {
-            const int64_t left = s < whole ? A::kStep : cut;
-            A::load(ap, a_off, a_end, left, a_held);
-            B::load(bp, b_off, b_end, left, b_held);
+            A::load(ap, a_off, a_ld, M - i0, left, (AA ? K : M) < 8, a_held);
+        }
+        if constexpr (BS == kStraight) {
+            if (s < whole) B::load(bp, b_off, to + A::kBytes);
+            else B::load_cut(bp, b_off, to + A::kBytes, cut);
+        } else {
+            B::load(bp, b_off, b_ld, N - j0, left, (BA ? K : N) < 8, b_held);
         }
         ap += A::step_bytes(a_ld);
         bp += B::step_bytes(b_ld);
     };
     auto settle = [&](int s, int buf) {
-        if constexpr (!BF) {
-            lds_char* to = lds + buf * S::kStepBytes;
-            const int64_t left = s < whole ? A::kStep : cut;
-            A::store(a_held, left, to);
-            B::store(b_held, left, to + A::kBytes);
-        }
+        lds_char* to = lds + buf * S::kStepBytes;
+        const int64_t left = K - (s0 + s) * A::kStep;
+        if constexpr (AS != kStraight) A::store(a_held, M - i0, left, (AA ? K : M) < 8, to);
+        if constexpr (BS != kStraight) B::store(b_held, N - j0, left, (BA ? K : N) < 8, to + A::kBytes);
         __builtin_amdgcn_s_waitcnt(kLandedAndRead);
     };
     auto read = [&](int buf, int h, Frag (&x)[MF], Frag (&y)[NF]) {
@@ -371,12 +435,12 @@ struct Choice {
 
 // The tile and the division of the contraction with the least expected time: steps of a tile one after the other, as many tiles
 // at a time as there are compute units, and the sums of the splits written and read again.
-Choice choose(bool bf16, int64_t M, int64_t N, int64_t K) {
+Choice choose(bool bf16, bool straight, int64_t M, int64_t N, int64_t K) {
     const int64_t steps = (K + (bf16 ? 63 : 31)) / (bf16 ? 64 : 32);
     Choice best{};
     double least = 0;
     for (int side : {256, 128, 64}) {
-        if (side == 256 && !bf16) continue;
+        if ((side == 256 && !straight) || (side > 64 && std::min(M, N) <= side / 2)) continue;
         const int64_t tm = (M + side - 1) / side, tn = (N + side - 1) / side, tiles = tm * tn;
         // us a step with the unit full, and at the least, of one tile by itself
         const double full = bf16 ? (side == 256 ? 1.46 : side == 128 ? 0.47 : 0.17) : (side == 128 ? 1.8 : 0.48);
@@ -397,10 +461,10 @@ Choice choose(bool bf16, int64_t M, int64_t N, int64_t K) {
     return best;
 }
 
-template <bool BF, bool AA, bool BA, int WM, int WN, int MF, int NF>
+template <bool BF, bool AA, bool BA, Source AS, Source BS, int WM, int WN, int MF, int NF>
 hipError_t start(const ProductCall& p, const Choice& ch) {
-    typedef Shape<BF, AA, BA, WM, WN, MF, NF> S;
-    auto k = k_product<BF, AA, BA, WM, WN, MF, NF>;
+    typedef Shape<BF, AA, BA, AS, BS, WM, WN, MF, NF> S;
+    auto k = k_product<BF, AA, BA, AS, BS, WM, WN, MF, NF>;
     if (S::kLds > 65536) {
         const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(k), hipFuncAttributeMaxDynamicSharedMemorySize, S::kLds);
         if (e != hipSuccess) return e;
@@ -411,10 +475,17 @@ hipError_t start(const ProductCall& p, const Choice& ch) {
     return hipGetLastError();
 }
 
-template <bool BF, int WM, int WN, int MF, int NF>
-hipError_t start_by_order(const ProductCall& p, const Choice& ch) {
-    if (p.a_along) return p.b_along ? start<BF, true, true, WM, WN, MF, NF>(p, ch) : start<BF, true, false, WM, WN, MF, NF>(p, ch);
-    return start<BF, false, false, WM, WN, MF, NF>(p, ch);
+template <bool BF, Source AS, Source BS>
+hipError_t start_by_shape(const ProductCall& p, const Choice& ch) {
+    auto by_side = [&](auto aa, auto ba) {
+        constexpr bool A = decltype(aa)::value, B = decltype(ba)::value;
+        if constexpr (BF && AS == kStraight)
+            if (ch.side == 256) return start<BF, A, B, AS, BS, 2, 4, 8, 4>(p, ch);
+        return ch.side == 128 ? start<BF, A, B, AS, BS, 2, 2, 4, 4>(p, ch) : start<BF, A, B, AS, BS, 2, 2, 2, 2>(p, ch);
+    };
+    if (p.a_along) return p.b_along ? by_side(std::true_type(), std::true_type()) : by_side(std::true_type(), std::false_type());
+    if constexpr (BF && BS == kFp32) return hipErrorInvalidValue;   // the weight gradient reads no weights
+    else return by_side(std::false_type(), std::false_type());
 }
 
 }  // namespace
@@ -425,12 +496,13 @@ int64_t product_partial_bytes(bool bf16, int64_t M, int64_t N, int64_t K) {
 }
 
 psgd_status launch_product(const ProductCall& p, std::string* what) {
-    const Choice ch = choose(p.bf16, p.M, p.N, p.K);
+    const bool straight = p.bf16 && p.a_ready && p.b_ready && !p.b_fp32;
+    const Choice ch = choose(p.bf16, straight, p.M, p.N, p.K);
     if (ch.tiles_m * ch.tiles_n * ch.splits > 0x7fffffffLL) return PSGD_EUNSUPPORTED;
     hipError_t e;
-    if (!p.bf16) e = ch.side == 128 ? start_by_order<false, 2, 2, 4, 4>(p, ch) : start_by_order<false, 2, 2, 2, 2>(p, ch);
-    else if (ch.side == 256) e = start_by_order<true, 2, 4, 8, 4>(p, ch);
-    else e = ch.side == 128 ? start_by_order<true, 2, 2, 4, 4>(p, ch) : start_by_order<true, 2, 2, 2, 2>(p, ch);
+    if (!p.bf16) e = start_by_shape<false, kFp32, kFp32>(p, ch);
+    else if (straight) e = start_by_shape<true, kStraight, kStraight>(p, ch);
+    else e = p.b_fp32 ? start_by_shape<true, kBf16, kFp32>(p, ch) : start_by_shape<true, kBf16, kBf16>(p, ch);
     if (e != hipSuccess) { *what = std::string("launch k_product: ") + hipGetErrorString(e); return PSGD_EHIP; }
     if (ch.splits > 1) {
         const int64_t blocks = (p.M * ((p.N + 7) / 8) + kBlock - 1) / kBlock;

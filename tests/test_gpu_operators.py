@@ -117,7 +117,8 @@ def near(got, want, bound):
 # sizes around the tiles' edges, rows of every alignment, one token to many, few features and many
 SIZES = [(1, 1, 2), (1, 512, 640), (2, 33, 17), (3, 130, 650), (7, 1000, 129), (8, 256, 1024), (16, 96, 4096), (17, 2048, 96),
          (31, 10, 512), (33, 64, 64), (64, 5, 40), (65, 257, 72), (100, 650, 130), (127, 128, 256), (128, 384, 128), (129, 255, 136),
-         (200, 264, 1000), (256, 256, 512), (257, 520, 264), (300, 1031, 48), (513, 768, 320), (1000, 136, 8)]
+         (200, 264, 1000), (256, 256, 512), (257, 520, 264), (300, 1031, 48), (513, 768, 320), (1000, 136, 8),
+         (40, 37, 43), (70, 9, 75), (66, 5, 7), (130, 3, 6), (300, 131, 263), (777, 333, 1001), (34, 1, 2), (90, 7, 1029)]
 TYPES = [("f32", "f32"), ("bf16", "bf16"), ("bf16", "f32")]
 
 
