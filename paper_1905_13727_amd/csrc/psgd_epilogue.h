@@ -96,7 +96,7 @@ __device__ __forceinline__ void slope_oct(const float (&z)[8], float (&v)[8], in
 }
 
 struct Epilogue {
-    int64_t row0;      // number of the first row, for the generator
+    int64_t row0, col0;   // numbers of the first row and column, for the generator (col0 a multiple of eight)
     float scale;
     const void* bias;
     int bias_bf, act;
@@ -116,7 +116,7 @@ inline DropArgs drop_of(const DropHost& h) {
     return d;
 }
 inline Epilogue epilogue_of(const EpilogueHost& h) {
-    return Epilogue{h.row0, h.scale, h.bias, h.bias_bf, h.act, h.pre, h.pre_ld, h.residual, h.residual_ld, drop_of(h.drop)};
+    return Epilogue{h.row0, h.col0, h.scale, h.bias, h.bias_bf, h.act, h.pre, h.pre_ld, h.residual, h.residual_ld, drop_of(h.drop)};
 }
 
 // Sixteen bytes that begin anywhere an element may: this generation's global accesses need no more than that, so rows of odd
@@ -177,7 +177,7 @@ __device__ __forceinline__ void finish_oct(const Epilogue& ep, const Draw& d, vo
     if (ep.pre) st_oct<BF>(ep.pre, pre_at, count, v);
     act_oct(v, ep.act);
     if (ep.drop.below) {
-        const Words r = philox(d, (unsigned)(j >> 3), (unsigned)(ep.row0 + i));
+        const Words r = philox(d, (unsigned)((ep.col0 + j) >> 3), (unsigned)(ep.row0 + i));
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = dropped(r, e, ep.drop.below) ? 0.f : v[e] * ep.drop.factor;
     }

@@ -13,7 +13,7 @@ namespace psgd {
 // What follows the sums, in this order: times scale, plus bias, stored as `pre`, activation, dropout, plus residual (or plus what C
 // holds: residual = C), stored.
 struct EpilogueHost {
-    int64_t row0 = 0;        // number of the first row, for dropout
+    int64_t row0 = 0, col0 = 0;   // numbers of the first row and column, for dropout
     float scale = 1.f;
     const void* bias = nullptr;
     bool bias_bf = false;

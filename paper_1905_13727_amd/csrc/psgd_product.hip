@@ -191,8 +191,9 @@ struct Operand {
             return *reinterpret_cast<const __attribute__((address_space(3))) Frag*>(s + row * 128 + (((4 * h + g) ^ (row & 7)) << 4));
         } else if constexpr (Z == 2) {
             // the four rows l .. l + 3 of a lane group's eight, sixteen outputs each: lane i asks for row i / 4, outputs 4 (i % 4)
-            const int l = 32 * h + 8 * g + (i >> 2), m = first + 16 * f + 4 * (i & 3);
-            const lds_char* p = s + l * (ROWS * Z) + ((((m * Z) >> 4) ^ key(l)) << 4) + ((m * Z) & 15);
+            // (first is a multiple of all the fragments' outputs, so that the fragment's number can go in by exclusive or)
+            const int l = 32 * h + 8 * g + (i >> 2), m = first + 4 * (i & 3);
+            const lds_char* p = s + l * (ROWS * Z) + ((((m * Z) >> 4) ^ key(l) ^ (2 * f)) << 4) + ((m * Z) & 15);
             typedef __attribute__((address_space(3))) v4s* lds_v4s;
             const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s)p);
             const v4s hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s)(p + 4 * (ROWS * Z)));   // key(l + 4) = key(l)
@@ -209,16 +210,20 @@ struct Operand {
 
 // ---- tiles ----------------------------------------------------------------------------------------------------------
 
+// s_waitcnt: no load (to LDS too) in flight and every LDS access done
+constexpr int kLandedAndRead = 0x0070;
+
 // The workgroups that run at the same time on one die (own L2) get neighbouring tiles: numbers are dealt to the eight dies in
 // ranges, and a range goes along the rows of C in bands of eight tiles.
-__device__ __forceinline__ void tile_of(int64_t number, int64_t count, int64_t tiles_m, int64_t tiles_n, int64_t& tm, int64_t& tn) {
-    const int64_t each = count / 8, more = count % 8, die = number % 8;
-    int64_t t = die * each + (die < more ? die : more) + number / 8;
-    constexpr int64_t kBand = 8;
-    const int64_t band = t / (kBand * tiles_n), first = band * kBand, high = tiles_m - first < kBand ? tiles_m - first : kBand;
-    t -= band * kBand * tiles_n;
-    tm = first + t % high;
+__device__ __forceinline__ void tile_of(int number, int count, int tiles_m, int tiles_n, int& tm, int& tn) {
+    const int each = count / 8, more = count % 8, die = number % 8;
+    int t = die * each + (die < more ? die : more) + number / 8;
+    constexpr int kBand = 8;
+    const int wide = kBand * tiles_n;
+    const int band = t / wide, first = band * kBand, high = tiles_m - first < kBand ? tiles_m - first : kBand;
+    t -= band * wide;
     tn = t / high;
+    tm = first + t - tn * high;
 }
 
 template <bool BF, bool AA, bool BA, Source AS, Source BS, int WM, int WN, int MF, int NF>
@@ -234,13 +239,10 @@ struct Shape {   // WM x WN waves, each MF x NF fragments of 16 x 16
     static_assert(kLds >= WM * WN * kPartBytes && MF % 2 == 0 && (NF == 4 || NF == 2), "32 rows of sums a wave");
 };
 
-// s_waitcnt: no load (to LDS too) in flight and every LDS access done
-constexpr int kLandedAndRead = 0x0070;
-
 // grid: tiles_m * tiles_n * splits.  With several splits of the contraction the sums go to `partial`, [split][M][N].
 template <bool BF, bool AA, bool BA, Source AS, Source BS, int WM, int WN, int MF, int NF>
 __global__ __launch_bounds__(WM* WN* kWave, 2) void k_product(const char* a, int64_t a_ld, const char* b, int64_t b_ld, void* c, int64_t c_ld,
-                                                             int64_t M, int64_t N, int64_t K, int64_t tiles_m, int64_t tiles_n,
+                                                             int64_t M, int64_t N, int64_t K, int tiles_m, int tiles_n,
                                                              int64_t steps_each, float* partial, Epilogue ep) {
     typedef Shape<BF, AA, BA, AS, BS, WM, WN, MF, NF> S;
     typedef typename S::A A;
@@ -248,10 +250,11 @@ __global__ __launch_bounds__(WM* WN* kWave, 2) void k_product(const char* a, int
     typedef typename S::Frag Frag;
     extern __shared__ __attribute__((aligned(16))) char lds_raw[];
     lds_char* const lds = (lds_char*)lds_raw;
-    int64_t tm, tn;
-    const int64_t tiles = tiles_m * tiles_n, split = blockIdx.x / tiles;
-    tile_of(blockIdx.x - split * tiles, tiles, tiles_m, tiles_n, tm, tn);
-    const int64_t i0 = tm * S::BM, j0 = tn * S::BN;
+    int tm, tn;
+    const int tiles = tiles_m * tiles_n;
+    const int64_t split = blockIdx.x / (unsigned)tiles;
+    tile_of((int)(blockIdx.x - (unsigned)split * tiles), tiles, tiles_m, tiles_n, tm, tn);
+    const int64_t i0 = (int64_t)tm * S::BM, j0 = (int64_t)tn * S::BN;
     const int64_t all = (K + A::kStep - 1) / A::kStep, s0 = split * steps_each;
     const int steps = (int)(s0 + steps_each < all ? steps_each : all - s0);
     const int cut = s0 + steps == all ? (int)(K % A::kStep) : 0;   // what the last step holds, if it is cut short
@@ -427,42 +430,69 @@ namespace {
 
 constexpr int kCUs = 256;
 
+// The tiles, and what they take: us a step with a unit full, of one tile by itself, and for first loads and epilogue; tiles that a
+// unit holds at once.  Measured on products of one to four rounds, 512 .. 16384 of the contraction.
+struct TileKind {
+    int side;
+    int at_once;
+    double full, alone, ends;
+};
+constexpr TileKind kTilesBf16[] = {{256, 1, 1.46, 1.46, 10}, {128, 2, 0.47, 0.7, 5}, {64, 4, 0.155, 0.5, 3}};
+constexpr TileKind kTilesFp32[] = {{0, 0, 0, 0, 0}, {128, 2, 1.9, 2.4, 5}, {64, 4, 0.5, 0.8, 3}};
+
 // A split takes four steps at least, and there are no more tiles and splits than the units hold at a time, so that the sums
 // take at most 64 MiB whatever the sizes.
 constexpr int64_t kMostSplits = 32, kLeastSteps = 4, kMostPartial = int64_t(kCUs) * 256 * 256 * 4;
-constexpr int64_t most_parts(int side) { return kCUs * (side == 64 ? 4 : side == 128 ? 2 : 1); }
-static_assert(most_parts(64) * 64 * 64 * 4 <= kMostPartial && most_parts(128) * 128 * 128 * 4 <= kMostPartial, "fits");
 
 struct Choice {
-    int side;          // tiles of side x side
+    int kind;          // of the tiles
     int64_t splits, steps_each, tiles_m, tiles_n;
     double us;         // expected
 };
 
 // The tile and the division of the contraction with the least expected time: steps of a tile one after the other, as many tiles
-// at a time as the units hold, and the sums of the splits written and read again.
+// at a time as the units hold, and the sums of the splits written and read again.  `straight`: both operands go straight to LDS.
 Choice choose(bool bf16, bool straight, int64_t M, int64_t N, int64_t K) {
     const int64_t steps = (K + (bf16 ? 63 : 31)) / (bf16 ? 64 : 32);
-    Choice best{};
-    for (int side : {256, 128, 64}) {
-        if ((side == 256 && !straight) || (side > 64 && std::min(M, N) <= side / 2)) continue;
-        const int64_t tm = (M + side - 1) / side, tn = (N + side - 1) / side, tiles = tm * tn;
-        // us a step and tile with the unit full, and a step of one tile by itself
-        const double full = bf16 ? (side == 256 ? 1.46 : side == 128 ? 0.47 : 0.155) : (side == 128 ? 1.9 : 0.5);
-        const double alone = bf16 ? (side == 256 ? 1.46 : side == 128 ? 0.7 : 0.5) : (side == 128 ? 2.4 : 0.8);
-        const double ends = side == 256 ? 10 : side == 128 ? 5 : 3;   // first loads, epilogue
-        const int64_t at_once = side == 256 ? 1 : side == 128 ? 2 : 4;
-        for (int64_t splits = 1; splits <= kMostSplits && (splits == 1 || (splits <= steps / kLeastSteps && tiles * splits <= most_parts(side))); ++splits) {
+    Choice best{-1, 0, 0, 0, 0, 0};
+    for (int kind = 0; kind < 3; ++kind) {
+        const TileKind& t = bf16 ? kTilesBf16[kind] : kTilesFp32[kind];
+        if (!t.side || (kind == 0 && !straight)) continue;
+        if (t.side > 64 && (M <= t.side / 2 || N <= t.side / 2)) continue;   // more than half of every tile outside
+        const int64_t tm = (M + t.side - 1) / t.side, tn = (N + t.side - 1) / t.side, tiles = tm * tn;
+        for (int64_t splits = 1; splits <= (kind == 0 ? 1 : kMostSplits) && (splits == 1 || (splits <= steps / kLeastSteps && tiles * splits <= kCUs * t.at_once)); ++splits) {
             const int64_t each = std::max<int64_t>(1, (steps + splits - 1) / splits), parts = std::max<int64_t>(1, (steps + each - 1) / each);
             if (parts != splits) continue;
             // tiles a unit works off: full loads, and what is left, which does not spread evenly
-            const int64_t n = tiles * splits, batches = n / (kCUs * at_once), rest = n % (kCUs * at_once);
-            const double left = rest == 0 ? 0 : std::max<double>((double)((rest + kCUs - 1) / kCUs), batches ? 0.8 * at_once : 0);
-            double us = each * std::max(alone, (batches * at_once + left) * full) + ends * (side == 256 ? batches + (rest > 0) : std::max<double>(1, (batches * at_once + left) / 2));
+            const int64_t n = tiles * splits, batches = n / (kCUs * t.at_once), rest = n % (kCUs * t.at_once);
+            const double left = rest == 0 ? 0 : std::max<double>((double)((rest + kCUs - 1) / kCUs), batches ? 0.8 * t.at_once : 0);
+            const double work = batches * t.at_once + left;
+            double us = each * std::max(t.alone, work * t.full) + t.ends * std::max<double>(1, work / std::min(t.at_once, 2));
             if (splits > 1) us += 4 + 2e-6 * splits * M * N;
-            if (best.side == 0 || us < best.us) best = Choice{side, splits, each, tm, tn, us};
+            if (best.kind < 0 || us < best.us) best = Choice{kind, splits, each, tm, tn, us};
         }
     }
+    return best;
+}
+
+// Rows (`rows`) or columns beyond the last full tile, and the expected time, if they are a product of their own; 0 if that is slower
+struct Rest {
+    int64_t count;
+    bool rows;
+    double us;
+};
+Rest rest_of(bool bf16, bool straight, int64_t M, int64_t N, int64_t K, double whole_us, bool columns_only) {
+    Rest best{0, false, 0.9 * whole_us};
+    for (int64_t side : {128, 256})
+        for (bool rows : {true, false}) {
+            const int64_t all = rows ? M : N, r = all % side;
+            if ((rows && columns_only) || r == 0 || r > side / 2 || all < side) continue;
+            const int64_t m = rows ? M - r : M, n = rows ? N : N - r;
+            double us = choose(bf16, straight, m, n, K).us;
+            if (rows) us = rest_of(bf16, straight, m, n, K, us, true).us / 0.9 < us ? rest_of(bf16, straight, m, n, K, us, true).us : us;
+            us += 2 + choose(bf16, straight, rows ? r : M, rows ? N : r, K).us;
+            if (us < best.us) best = Rest{r, rows, us};
+        }
     return best;
 }
 
@@ -475,7 +505,7 @@ hipError_t start(const ProductCall& p, const Choice& ch) {
         if (e != hipSuccess) return e;
     }
     hipLaunchKernelGGL(k, dim3((unsigned)(ch.tiles_m * ch.tiles_n * ch.splits)), dim3(S::T), S::kLds, p.stream, static_cast<const char*>(p.a), p.a_ld,
-                       static_cast<const char*>(p.b), p.b_ld, p.c, p.c_ld, p.M, p.N, p.K, ch.tiles_m, ch.tiles_n, ch.steps_each,
+                       static_cast<const char*>(p.b), p.b_ld, p.c, p.c_ld, p.M, p.N, p.K, (int)ch.tiles_m, (int)ch.tiles_n, ch.steps_each,
                        ch.splits > 1 ? p.partial : nullptr, epilogue_of(p.ep));
     return hipGetLastError();
 }
@@ -485,8 +515,8 @@ hipError_t start_by_shape(const ProductCall& p, const Choice& ch) {
     auto by_side = [&](auto aa, auto ba) {
         constexpr bool A = decltype(aa)::value, B = decltype(ba)::value;
         if constexpr (BF && AS == kStraight)
-            if (ch.side == 256) return start<BF, A, B, AS, BS, 2, 4, 8, 4>(p, ch);
-        return ch.side == 128 ? start<BF, A, B, AS, BS, 2, 2, 4, 4>(p, ch) : start<BF, A, B, AS, BS, 2, 2, 2, 2>(p, ch);
+            if (ch.kind == 0) return start<BF, A, B, AS, BS, 2, 4, 8, 4>(p, ch);
+        return ch.kind == 1 ? start<BF, A, B, AS, BS, 2, 2, 4, 4>(p, ch) : start<BF, A, B, AS, BS, 2, 2, 2, 2>(p, ch);
     };
     if (p.a_along) return p.b_along ? by_side(std::true_type(), std::true_type()) : by_side(std::true_type(), std::false_type());
     if constexpr (BF && BS == kFp32) return hipErrorInvalidValue;   // the weight gradient reads no weights
@@ -504,23 +534,29 @@ psgd_status launch_product(const ProductCall& p, std::string* what) {
     const bool straight = p.bf16 && p.a_ready && p.b_ready && !p.b_fp32;
     const Choice ch = choose(p.bf16, straight, p.M, p.N, p.K);
     if (ch.tiles_m * ch.tiles_n * ch.splits > 0x7fffffffLL) return PSGD_EUNSUPPORTED;
-    // Rows beyond the last full tile cost a row of tiles, which may be the one too many for the last round: a product of their own, in
-    // small tiles, where that is expected to be faster by a tenth.  4099 x 2048 x 8192 bf16 205 us in one, ...
-    const int64_t rest = p.M % 128;
-    if (rest > 0 && rest <= 64 && p.M > 128) {
-        const Choice body = choose(p.bf16, straight, p.M - rest, p.N, p.K), tail = choose(p.bf16, straight, rest, p.N, p.K);
-        if (body.us + tail.us + 2 < 0.9 * ch.us) {
+    // Rows or columns beyond the last full tile cost a row of tiles, which may be the one too many for the last round: a product of
+    // their own, in small tiles, where that is expected to be faster by a tenth.  4099 x 2048 x 8192 bf16 205 us in one, 149 in two.
+    if (ch.us > 30) {
+        const Rest over = rest_of(p.bf16, straight, p.M, p.N, p.K, ch.us, false);
+        const int64_t rest = over.count;
+        const bool rows = over.rows;
+        if (rest) {
+            const int64_t z = p.bf16 ? 2 : 4, zb = p.bf16 && !p.b_fp32 ? 2 : 4, zp = p.ep.bias_bf ? 2 : 4;
             ProductCall q = p;
-            q.M = p.M - rest;
+            (rows ? q.M : q.N) -= rest;
             const psgd_status st = launch_product(q, what);
             if (st != PSGD_OK) return st;
-            const int64_t z = p.bf16 ? 2 : 4, row = q.M;
-            q.M = rest;
+            const int64_t row = rows ? q.M : 0, col = rows ? 0 : q.N;
+            (rows ? q.M : q.N) = rest;
+            auto moved = [&](const void* at, int64_t ld, int64_t size) { return at ? static_cast<const char*>(at) + (row * ld + col) * size : nullptr; };
             q.a = static_cast<const char*>(p.a) + (p.a_along ? row * p.a_ld : row) * z;
-            q.c = static_cast<char*>(p.c) + row * p.c_ld * z;
-            if (p.ep.pre) q.ep.pre = static_cast<char*>(p.ep.pre) + row * p.ep.pre_ld * z;
-            if (p.ep.residual) q.ep.residual = static_cast<const char*>(p.ep.residual) + row * p.ep.residual_ld * z;
+            q.b = static_cast<const char*>(p.b) + (p.b_along ? col * p.b_ld : col) * zb;
+            q.c = const_cast<char*>(moved(p.c, p.c_ld, z));
+            q.ep.pre = const_cast<char*>(moved(p.ep.pre, p.ep.pre_ld, z));
+            q.ep.residual = moved(p.ep.residual, p.ep.residual_ld, z);
+            if (p.ep.bias) q.ep.bias = static_cast<const char*>(p.ep.bias) + col * zp;
             q.ep.row0 = p.ep.row0 + row;
+            q.ep.col0 = p.ep.col0 + col;
             return launch_product(q, what);
         }
     }

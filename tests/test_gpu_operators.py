@@ -322,6 +322,26 @@ def test_rows_do_not_depend_on_the_others_mask():
     assert all(torch.equal(ys[-1][:m.shape[0]], m) for m in ys)
 
 
+@pytest.mark.parametrize("dtype,params", TYPES)
+@pytest.mark.parametrize("T,n,k", [(1027, 2064, 1032), (2055, 2049, 520), (1100, 2180, 1028), (530, 8200, 520), (4100, 520, 1100)])
+def test_large_products_with_something_over(T, n, k, dtype, params):
+    """Large enough that rows and columns beyond the last tile become products of their own: with everything behind the product,
+    and backward."""
+    dev = _need_gpu()
+    L = Layer(n, k, dtype, params, dev)
+    x, res = L.normal(T, k), L.normal(T, n)
+    y, pre, ws = Rows(T, n, DT[dtype], dev, 3, 1), Rows(T, n, DT[dtype], dev), L.workspace(T)
+    L.plan.linear_forward(1, T, L.param, x, y.ptr(), ws, residual=res, pre=pre.ptr(), activation="gelu_tanh", drop=0.3, rng=_rng(dev),
+                          offset=SHIFT, y_stride=y.ld, **L.op())
+    X, W, b, R = _f64(x), L.weight(), L.bias_values(), _f64(res)
+    factor = OO.drop_factor(T, n, 0.3, SEED, OFFSET + SHIFT)
+    want, z = OO.linear_forward(X, W, b, "gelu_tanh", factor, R)
+    near(y.view(), want, forward_bound(X, W, z, b, "gelu_tanh", factor, R, dtype, k))
+    near(pre.view(), z, forward_bound(X, W, z, b, "identity", 1.0, None, dtype, k))
+    assert y.around_is_untouched() and pre.around_is_untouched()
+    run_backward(L, T, "gelu_tanh", 0.3, accumulate=True)
+
+
 def test_outputs_beyond_32_bit_offsets():
     """[70000][33280] bf16 outputs (4.7 GB) over eight columns of input: rows at both ends and behind 2^31 elements, backward too."""
     dev = _need_gpu()
