@@ -74,23 +74,6 @@ __global__ __launch_bounds__(kBlock) void k_dz(const void* dy, int64_t dy_ld, co
     partial[bt * n + col] = v;
 }
 
-// db from the blocks' sums: a workgroup 64 columns, its four waves every fourth block, joined in order
-template <bool BF>
-__global__ __launch_bounds__(kBlock) void k_column_sum(const float* partial, int64_t count, int64_t n, float scale, void* db, int accumulate) {
-    __shared__ float sums[4][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t col = (int64_t)blockIdx.x * 64 + lane;
-    float v = 0.f;
-    if (col < n)
-        for (int64_t i = wave; i < count; i += 4) v += partial[i * n + col];
-    sums[wave][lane] = v;
-    __syncthreads();
-    if (wave || col >= n) return;
-    v = ((sums[0][lane] + sums[1][lane]) + (sums[2][lane] + sums[3][lane])) * scale;
-    if (accumulate) v += ld_any(db, col, BF);
-    st_any(db, col, v, BF);
-}
-
 namespace {
 
 int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b * b; }
@@ -172,8 +155,8 @@ bool input(const LinearCall& c, const Parts& p, const ProductCall& q, const void
 
 int64_t linear_workspace_bytes(const LinearCall& c) {
     if (c.T == 0) return 0;
-    return parts_of(c).partial + std::max({product_partial_bytes(c.bf16, c.T, c.n, c.k), product_partial_bytes(c.bf16, c.T, c.k, c.n),
-                                           product_partial_bytes(c.bf16, c.n, c.k, c.T)});
+    return parts_of(c).partial + std::max(product_partial_bytes(c.bf16, c.T, c.n, c.k),
+                                          up(product_partial_bytes(c.bf16, c.T, c.k, c.n), 256) + product_partial_bytes(c.bf16, c.n, c.k, c.T));
 }
 
 psgd_status launch_linear_forward(const LinearCall& c, std::string* what) {
@@ -228,46 +211,39 @@ psgd_status launch_linear_backward(const LinearCall& c, std::string* what) {
             if (failed("k_dz", what)) return PSGD_EHIP;
         }
     }
-    if (c.db) {
-        auto k = c.bf16 ? k_column_sum<true> : k_column_sum<false>;
-        hipLaunchKernelGGL(k, dim3((unsigned)((c.n + 63) / 64)), dim3(kBlock), 0, s, reinterpret_cast<const float*>(ws + p.db), blocks, c.n, scale,
-                           c.db, (int)c.accumulate);
-        if (failed("k_column_sum", what)) return PSGD_EHIP;
-    }
-    ProductCall q{};
-    q.bf16 = c.bf16;
-    q.ep.scale = scale;
-    q.partial = reinterpret_cast<float*>(ws + p.partial);
-    q.stream = s;
-    q.a = dz;
-    q.a_ld = dz_ld;
-    q.a_ready = dz_ready;
-    q.N = c.k;
-    if (c.dx && c.T > 0) {
-        q.a_along = true;
-        q.c = c.dx;
-        q.c_ld = c.dx_ld;
-        q.M = c.T;
-        q.K = c.n;
-        if (!weights(c, p, q, what)) return PSGD_EHIP;
-        const psgd_status st = launch_product(q, what);
-        if (st != PSGD_OK) return st;
+    const ColumnSums sums{reinterpret_cast<const float*>(ws + p.db), blocks, c.n, scale, c.db, (int)c.accumulate};
+    ProductCall x{};
+    x.bf16 = c.bf16;
+    x.ep.scale = scale;
+    x.partial = reinterpret_cast<float*>(ws + p.partial);
+    x.stream = s;
+    x.a = dz;
+    x.a_ld = dz_ld;
+    x.a_ready = dz_ready;
+    x.N = c.k;
+    ProductCall w = x;
+    const bool want_x = c.dx && c.T > 0;
+    if (want_x) {
+        x.a_along = true;
+        x.c = c.dx;
+        x.c_ld = c.dx_ld;
+        x.M = c.T;
+        x.K = c.n;
+        if (!weights(c, p, x, what)) return PSGD_EHIP;
+        w.partial += up(product_partial_bytes(c.bf16, c.T, c.k, c.n), 256) / 4;
     }
     if (c.dw) {
-        q.a_along = false;
-        q.b_fp32 = false;
-        q.c = c.dw;
-        q.c_ld = c.k;
-        q.M = c.n;
-        q.K = c.T;
-        if (!input(c, p, q, &q.b, &q.b_ld, &q.b_ready, what)) return PSGD_EHIP;
+        w.c = c.dw;
+        w.c_ld = c.k;
+        w.M = c.n;
+        w.K = c.T;
+        if (!input(c, p, w, &w.b, &w.b_ld, &w.b_ready, what)) return PSGD_EHIP;
         if (c.accumulate) {
-            q.ep.residual = c.dw;
-            q.ep.residual_ld = c.k;
+            w.ep.residual = c.dw;
+            w.ep.residual_ld = c.k;
         }
-        return launch_product(q, what);
     }
-    return PSGD_OK;
+    return launch_backward_products(want_x ? &x : nullptr, c.dw ? &w : nullptr, c.db ? &sums : nullptr, what);
 }
 
 }  // namespace psgd

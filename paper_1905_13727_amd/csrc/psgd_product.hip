@@ -226,6 +226,16 @@ __device__ __forceinline__ void tile_of(int number, int count, int tiles_m, int 
     tm = first + t - tn * high;
 }
 
+struct ProductArgs {
+    const char *a, *b;
+    int64_t a_ld, b_ld;
+    void* c;
+    int64_t c_ld, M, N, K;
+    int tiles_m, tiles_n, steps_each, splits;
+    float* partial;          // [split][M][N], with several splits of the contraction
+    Epilogue ep;
+};
+
 template <bool BF, bool AA, bool BA, Source AS, Source BS, int WM, int WN, int MF, int NF>
 struct Shape {   // WM x WN waves, each MF x NF fragments of 16 x 16
     static constexpr int BM = WM * MF * 16, BN = WN * NF * 16, T = WM * WN * kWave;
@@ -239,24 +249,28 @@ struct Shape {   // WM x WN waves, each MF x NF fragments of 16 x 16
     static_assert(kLds >= WM * WN * kPartBytes && MF % 2 == 0 && (NF == 4 || NF == 2), "32 rows of sums a wave");
 };
 
-// grid: tiles_m * tiles_n * splits.  With several splits of the contraction the sums go to `partial`, [split][M][N].
+// Tile and split number `block` of tiles_m * tiles_n * splits
 template <bool BF, bool AA, bool BA, Source AS, Source BS, int WM, int WN, int MF, int NF>
-__global__ __launch_bounds__(WM* WN* kWave, 2) void k_product(const char* a, int64_t a_ld, const char* b, int64_t b_ld, void* c, int64_t c_ld,
-                                                             int64_t M, int64_t N, int64_t K, int tiles_m, int tiles_n,
-                                                             int64_t steps_each, float* partial, Epilogue ep) {
+__device__ __forceinline__ void product_tile(const ProductArgs& p, unsigned block, char* lds_raw) {
+    const char *const a = p.a, *const b = p.b;
+    const int64_t a_ld = p.a_ld, b_ld = p.b_ld, M = p.M, N = p.N, K = p.K;
+    const int tiles_m = p.tiles_m, tiles_n = p.tiles_n;
+    void* const c = p.c;
+    int64_t c_ld = p.c_ld;
+    float* const partial = p.partial;
+    const Epilogue& ep = p.ep;
     typedef Shape<BF, AA, BA, AS, BS, WM, WN, MF, NF> S;
     typedef typename S::A A;
     typedef typename S::B B;
     typedef typename S::Frag Frag;
-    extern __shared__ __attribute__((aligned(16))) char lds_raw[];
     lds_char* const lds = (lds_char*)lds_raw;
     int tm, tn;
     const int tiles = tiles_m * tiles_n;
-    const int64_t split = blockIdx.x / (unsigned)tiles;
-    tile_of((int)(blockIdx.x - (unsigned)split * tiles), tiles, tiles_m, tiles_n, tm, tn);
+    const int64_t split = block / (unsigned)tiles;
+    tile_of((int)(block - (unsigned)split * tiles), tiles, tiles_m, tiles_n, tm, tn);
     const int64_t i0 = (int64_t)tm * S::BM, j0 = (int64_t)tn * S::BN;
-    const int64_t all = (K + A::kStep - 1) / A::kStep, s0 = split * steps_each;
-    const int steps = (int)(s0 + steps_each < all ? steps_each : all - s0);
+    const int64_t all = (K + A::kStep - 1) / A::kStep, s0 = split * p.steps_each;
+    const int steps = (int)(s0 + p.steps_each < all ? p.steps_each : all - s0);
     const int cut = s0 + steps == all ? (int)(K % A::kStep) : 0;   // what the last step holds, if it is cut short
     const int whole = steps - (cut ? 1 : 0);
 
@@ -400,30 +414,75 @@ __global__ __launch_bounds__(WM* WN* kWave, 2) void k_product(const char* a, int
     }
 }
 
+template <bool BF, bool AA, bool BA, Source AS, Source BS, int WM, int WN, int MF, int NF>
+__global__ __launch_bounds__(WM* WN* kWave, 2) void k_product(ProductArgs p) {
+    extern __shared__ __attribute__((aligned(16))) char lds_raw[];
+    product_tile<BF, AA, BA, AS, BS, WM, WN, MF, NF>(p, blockIdx.x, lds_raw);
+}
+
+// The input gradient (`first` workgroups) and the weight gradient of a layer in one launch: neither waits for the other, and small
+// ones fill the chip together
+template <bool BF, Source AS, Source BS, Source BS2, int WM, int WN, int MF, int NF>
+__global__ __launch_bounds__(WM* WN* kWave, 2) void k_product_two(ProductArgs p, ProductArgs q, unsigned first) {
+    extern __shared__ __attribute__((aligned(16))) char lds_raw[];
+    if (blockIdx.x < first) product_tile<BF, true, false, AS, BS, WM, WN, MF, NF>(p, blockIdx.x, lds_raw);
+    else product_tile<BF, false, false, AS, BS2, WM, WN, MF, NF>(q, blockIdx.x - first, lds_raw);
+}
+
 // The sum over the splits, in order, and the epilogue.  One lane: eight columns.
 template <bool BF>
-__global__ __launch_bounds__(kWave) void k_join(const float* partial, int64_t splits, void* c, int64_t c_ld, int64_t M, int64_t N,
-                                                 Epilogue ep) {
-    const int64_t per_row = (N + 7) / 8, at = (int64_t)blockIdx.x * kWave + threadIdx.x;
+__device__ __forceinline__ void join_octs(const ProductArgs& p, int64_t block) {
+    const int64_t per_row = (p.N + 7) / 8, at = block * kWave + threadIdx.x;
     Draw d{};
-    if (ep.drop.below) d = make_draw(ep.drop.rng, ep.drop.offset);
-    if (at >= M * per_row) return;
+    if (p.ep.drop.below) d = make_draw(p.ep.drop.rng, p.ep.drop.offset);
+    if (at >= p.M * per_row) return;
     const int64_t i = at / per_row, j = 8 * (at - i * per_row);
-    const int count = N - j < 8 ? (int)(N - j) : 8;
+    const int count = p.N - j < 8 ? (int)(p.N - j) : 8;
     float v[8] = {}, bias[8];
-    bias_oct(ep, j, N, bias);
-    for (int64_t s = 0; s < splits; s += 8) {   // eight splits' loads in flight, added in order
+    bias_oct(p.ep, j, p.N, bias);
+    for (int s = 0; s < p.splits; s += 8) {   // eight splits' loads in flight, added in order
         float x[8][8];
 #pragma unroll
         for (int q = 0; q < 8; ++q)
-            if (s + q < splits) ld_oct<false>(partial, ((s + q) * M + i) * N + j, count, x[q]);
+            if (s + q < p.splits) ld_oct<false>(p.partial, ((s + q) * p.M + i) * p.N + j, count, x[q]);
 #pragma unroll
         for (int q = 0; q < 8; ++q)
-            if (s + q < splits)
+            if (s + q < p.splits)
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[e] += x[q][e];
     }
-    finish_oct<BF>(ep, d, c, i * c_ld + j, i * ep.pre_ld + j, i * ep.residual_ld + j, i, j, count, v, bias);
+    finish_oct<BF>(p.ep, d, p.c, i * p.c_ld + j, i * p.ep.pre_ld + j, i * p.ep.residual_ld + j, i, j, count, v, bias);
+}
+
+// Sixteen columns of the blocks' column sums: four lanes a column take every fourth block, eight in flight, and are added in order
+template <bool BF>
+__device__ __forceinline__ void column_sums(const ColumnSums& s, int64_t block) {
+    __shared__ float part[4][16];
+    const int lc = threadIdx.x & 15, lg = threadIdx.x >> 4;
+    const int64_t col = block * 16 + lc;
+    float v = 0.f;
+    if (col < s.n)
+        for (int64_t i = lg; i < s.count; i += 32) {
+            float x[8];
+#pragma unroll
+            for (int q = 0; q < 8; ++q) x[q] = i + 4 * q < s.count ? s.sums[(i + 4 * q) * s.n + col] : 0.f;
+#pragma unroll
+            for (int q = 0; q < 8; ++q) v += x[q];
+        }
+    part[lg][lc] = v;
+    __syncthreads();
+    if (lg || col >= s.n) return;
+    v = ((part[0][lc] + part[1][lc]) + (part[2][lc] + part[3][lc])) * s.scale;
+    if (s.accumulate) v += ld_any(s.db, col, BF);
+    st_any(s.db, col, v, BF);
+}
+
+// What is left to add up behind the products of one call: the splits of up to two, and the bias gradient
+template <bool BF>
+__global__ __launch_bounds__(kWave) void k_join(ProductArgs p, int64_t p_blocks, ProductArgs q, int64_t q_blocks, ColumnSums s) {
+    if (blockIdx.x < p_blocks) join_octs<BF>(p, blockIdx.x);
+    else if (blockIdx.x < p_blocks + q_blocks) join_octs<BF>(q, blockIdx.x - p_blocks);
+    else column_sums<BF>(s, blockIdx.x - p_blocks - q_blocks);
 }
 
 namespace {
@@ -452,13 +511,13 @@ struct Choice {
 
 // The tile and the division of the contraction with the least expected time: steps of a tile one after the other, as many tiles
 // at a time as the units hold, and the sums of the splits written and read again.  `straight`: both operands go straight to LDS.
-Choice choose(bool bf16, bool straight, int64_t M, int64_t N, int64_t K) {
+Choice choose(bool bf16, bool straight, int64_t M, int64_t N, int64_t K, int only = -1) {
     const int64_t steps = (K + (bf16 ? 63 : 31)) / (bf16 ? 64 : 32);
     Choice best{-1, 0, 0, 0, 0, 0};
     for (int kind = 0; kind < 3; ++kind) {
         const TileKind& t = bf16 ? kTilesBf16[kind] : kTilesFp32[kind];
-        if (!t.side || (kind == 0 && !straight)) continue;
-        if (t.side > 64 && (M <= t.side / 2 || N <= t.side / 2)) continue;   // more than half of every tile outside
+        if (!t.side || (kind == 0 && !straight) || (only >= 0 && kind != only)) continue;
+        if (only < 0 && t.side > 64 && (M <= t.side / 2 || N <= t.side / 2)) continue;   // more than half of every tile outside
         const int64_t tm = (M + t.side - 1) / t.side, tn = (N + t.side - 1) / t.side, tiles = tm * tn;
         for (int64_t splits = 1; splits <= (kind == 0 ? 1 : kMostSplits) && (splits == 1 || (splits <= steps / kLeastSteps && tiles * splits <= kCUs * t.at_once)); ++splits) {
             const int64_t each = std::max<int64_t>(1, (steps + splits - 1) / splits), parts = std::max<int64_t>(1, (steps + each - 1) / each);
@@ -496,31 +555,73 @@ Rest rest_of(bool bf16, bool straight, int64_t M, int64_t N, int64_t K, double w
     return best;
 }
 
+ProductArgs args_of(const ProductCall& p, const Choice& ch) {
+    return ProductArgs{static_cast<const char*>(p.a), static_cast<const char*>(p.b), p.a_ld, p.b_ld, p.c, p.c_ld, p.M, p.N, p.K, (int)ch.tiles_m,
+                       (int)ch.tiles_n, (int)ch.steps_each, (int)ch.splits, ch.splits > 1 ? p.partial : nullptr, epilogue_of(p.ep)};
+}
+
+// More than 64 KB of LDS has to be asked for
+template <typename Kernel>
+hipError_t with_lds(Kernel k, int bytes) {
+    return bytes > 65536 ? hipFuncSetAttribute(reinterpret_cast<const void*>(k), hipFuncAttributeMaxDynamicSharedMemorySize, bytes) : hipSuccess;
+}
+
 template <bool BF, bool AA, bool BA, Source AS, Source BS, int WM, int WN, int MF, int NF>
-hipError_t start(const ProductCall& p, const Choice& ch) {
+hipError_t start(const ProductArgs& p, hipStream_t stream) {
     typedef Shape<BF, AA, BA, AS, BS, WM, WN, MF, NF> S;
     auto k = k_product<BF, AA, BA, AS, BS, WM, WN, MF, NF>;
-    if (S::kLds > 65536) {
-        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(k), hipFuncAttributeMaxDynamicSharedMemorySize, S::kLds);
-        if (e != hipSuccess) return e;
-    }
-    hipLaunchKernelGGL(k, dim3((unsigned)(ch.tiles_m * ch.tiles_n * ch.splits)), dim3(S::T), S::kLds, p.stream, static_cast<const char*>(p.a), p.a_ld,
-                       static_cast<const char*>(p.b), p.b_ld, p.c, p.c_ld, p.M, p.N, p.K, (int)ch.tiles_m, (int)ch.tiles_n, ch.steps_each,
-                       ch.splits > 1 ? p.partial : nullptr, epilogue_of(p.ep));
+    const hipError_t e = with_lds(k, S::kLds);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(k, dim3((unsigned)(p.tiles_m * p.tiles_n * p.splits)), dim3(S::T), S::kLds, stream, p);
     return hipGetLastError();
 }
 
 template <bool BF, Source AS, Source BS>
 hipError_t start_by_shape(const ProductCall& p, const Choice& ch) {
+    const ProductArgs d = args_of(p, ch);
     auto by_side = [&](auto aa, auto ba) {
         constexpr bool A = decltype(aa)::value, B = decltype(ba)::value;
         if constexpr (BF && AS == kStraight)
-            if (ch.kind == 0) return start<BF, A, B, AS, BS, 2, 4, 8, 4>(p, ch);
-        return ch.kind == 1 ? start<BF, A, B, AS, BS, 2, 2, 4, 4>(p, ch) : start<BF, A, B, AS, BS, 2, 2, 2, 2>(p, ch);
+            if (ch.kind == 0) return start<BF, A, B, AS, BS, 2, 4, 8, 4>(d, p.stream);
+        return ch.kind == 1 ? start<BF, A, B, AS, BS, 2, 2, 4, 4>(d, p.stream) : start<BF, A, B, AS, BS, 2, 2, 2, 2>(d, p.stream);
     };
     if (p.a_along) return p.b_along ? by_side(std::true_type(), std::true_type()) : by_side(std::true_type(), std::false_type());
     if constexpr (BF && BS == kFp32) return hipErrorInvalidValue;   // the weight gradient reads no weights
     else return by_side(std::false_type(), std::false_type());
+}
+
+template <bool BF, Source AS, Source BS, Source BS2>
+hipError_t start_two(const ProductArgs& p, const ProductArgs& q, int kind, hipStream_t stream) {
+    auto go = [&](auto k, auto shape) {
+        typedef decltype(shape) S;
+        const unsigned first = (unsigned)(p.tiles_m * p.tiles_n * p.splits);
+        const hipError_t e = with_lds(k, S::kLds);
+        if (e != hipSuccess) return e;
+        hipLaunchKernelGGL(k, dim3(first + (unsigned)(q.tiles_m * q.tiles_n * q.splits)), dim3(S::T), S::kLds, stream, p, q, first);
+        return hipGetLastError();
+    };
+    return kind == 1 ? go(k_product_two<BF, AS, BS, BS2, 2, 2, 4, 4>, Shape<BF, true, false, AS, BS, 2, 2, 4, 4>())
+                     : go(k_product_two<BF, AS, BS, BS2, 2, 2, 2, 2>, Shape<BF, true, false, AS, BS, 2, 2, 2, 2>());
+}
+
+bool is_straight(const ProductCall& p) { return p.bf16 && p.a_ready && p.b_ready && !p.b_fp32; }
+int64_t join_blocks(const ProductArgs& p) { return p.partial ? (p.M * ((p.N + 7) / 8) + kWave - 1) / kWave : 0; }
+
+psgd_status join(bool bf16, const ProductArgs& p, const ProductArgs& q, const ColumnSums* sums, hipStream_t stream, std::string* what) {
+    const int64_t pb = join_blocks(p), qb = join_blocks(q), sb = sums ? (sums->n + 15) / 16 : 0;
+    if (pb + qb + sb == 0) return PSGD_OK;
+    auto k = bf16 ? k_join<true> : k_join<false>;
+    hipLaunchKernelGGL(k, dim3((unsigned)(pb + qb + sb)), dim3(kWave), 0, stream, p, pb, q, qb, sums ? *sums : ColumnSums{});
+    const hipError_t e = hipGetLastError();
+    if (e == hipSuccess) return PSGD_OK;
+    *what = std::string("launch k_join: ") + hipGetErrorString(e);
+    return PSGD_EHIP;
+}
+
+psgd_status product_failed(hipError_t e, std::string* what) {
+    if (e == hipSuccess) return PSGD_OK;
+    *what = std::string("launch k_product: ") + hipGetErrorString(e);
+    return PSGD_EHIP;
 }
 
 }  // namespace
@@ -531,7 +632,7 @@ int64_t product_partial_bytes(bool bf16, int64_t M, int64_t N, int64_t K) {
 }
 
 psgd_status launch_product(const ProductCall& p, std::string* what) {
-    const bool straight = p.bf16 && p.a_ready && p.b_ready && !p.b_fp32;
+    const bool straight = is_straight(p);
     const Choice ch = choose(p.bf16, straight, p.M, p.N, p.K);
     if (ch.tiles_m * ch.tiles_n * ch.splits > 0x7fffffffLL) return PSGD_EUNSUPPORTED;
     // Rows or columns beyond the last full tile cost a row of tiles, which may be the one too many for the last round: a product of
@@ -560,19 +661,42 @@ psgd_status launch_product(const ProductCall& p, std::string* what) {
             return launch_product(q, what);
         }
     }
-    hipError_t e;
-    if (!p.bf16) e = start_by_shape<false, kFp32, kFp32>(p, ch);
-    else if (straight) e = start_by_shape<true, kStraight, kStraight>(p, ch);
-    else e = p.b_fp32 ? start_by_shape<true, kBf16, kFp32>(p, ch) : start_by_shape<true, kBf16, kBf16>(p, ch);
-    if (e != hipSuccess) { *what = std::string("launch k_product: ") + hipGetErrorString(e); return PSGD_EHIP; }
-    if (ch.splits > 1) {
-        const int64_t blocks = (p.M * ((p.N + 7) / 8) + kWave - 1) / kWave;
-        auto k = p.bf16 ? k_join<true> : k_join<false>;
-        hipLaunchKernelGGL(k, dim3((unsigned)blocks), dim3(kWave), 0, p.stream, p.partial, ch.splits, p.c, p.c_ld, p.M, p.N, epilogue_of(p.ep));
-        e = hipGetLastError();
-        if (e != hipSuccess) { *what = std::string("launch k_join: ") + hipGetErrorString(e); return PSGD_EHIP; }
+    const psgd_status st = product_failed(!p.bf16 ? start_by_shape<false, kFp32, kFp32>(p, ch) : straight ? start_by_shape<true, kStraight, kStraight>(p, ch)
+                                          : p.b_fp32 ? start_by_shape<true, kBf16, kFp32>(p, ch) : start_by_shape<true, kBf16, kBf16>(p, ch), what);
+    return st != PSGD_OK ? st : join(p.bf16, args_of(p, ch), ProductArgs{}, nullptr, p.stream, what);
+}
+
+psgd_status launch_backward_products(const ProductCall* x, const ProductCall* w, const ColumnSums* sums, std::string* what) {
+    if (x && w) {
+        // In one launch where both take the same tiles and neither has rows or columns over: worth a tile that is not each one's best
+        // if what that costs is less than the launch.
+        const bool sx = is_straight(*x), sw = is_straight(*w);
+        Choice cx = choose(x->bf16, sx, x->M, x->N, x->K), cw = choose(w->bf16, sw, w->M, w->N, w->K);
+        if (cx.us + cw.us < 150 && (cx.kind != cw.kind || cx.kind == 0)) {
+            double least = cx.us + cw.us + 4;
+            for (int kind : {1, 2}) {
+                const Choice tx = choose(x->bf16, sx, x->M, x->N, x->K, kind), tw = choose(w->bf16, sw, w->M, w->N, w->K, kind);
+                if (tx.us + tw.us < least) least = tx.us + tw.us, cx = tx, cw = tw;
+            }
+        }
+        const int64_t blocks = cx.tiles_m * cx.tiles_n * cx.splits + cw.tiles_m * cw.tiles_n * cw.splits;
+        if (cx.kind == cw.kind && cx.kind > 0 && cx.us + cw.us < 150 && blocks < 0x7fffffffLL) {
+            const ProductArgs p = args_of(*x, cx), q = args_of(*w, cw);
+            const hipError_t e = !x->bf16 ? start_two<false, kFp32, kFp32, kFp32>(p, q, cx.kind, x->stream)
+                                 : sx && sw ? start_two<true, kStraight, kStraight, kStraight>(p, q, cx.kind, x->stream)
+                                 : x->b_fp32 ? start_two<true, kBf16, kFp32, kBf16>(p, q, cx.kind, x->stream)
+                                             : start_two<true, kBf16, kBf16, kBf16>(p, q, cx.kind, x->stream);
+            const psgd_status st = product_failed(e, what);
+            return st != PSGD_OK ? st : join(x->bf16, p, q, sums, x->stream, what);
+        }
     }
-    return PSGD_OK;
+    for (const ProductCall* p : {x, w})
+        if (p) {
+            const psgd_status st = launch_product(*p, what);
+            if (st != PSGD_OK) return st;
+        }
+    const ProductCall* any = x ? x : w;
+    return sums ? join(any->bf16, ProductArgs{}, ProductArgs{}, sums, any->stream, what) : PSGD_OK;
 }
 
 }  // namespace psgd
