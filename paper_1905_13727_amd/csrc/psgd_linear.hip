@@ -24,8 +24,6 @@ __global__ __launch_bounds__(kBlock) void k_lay_out(const void* src, int64_t src
 // dz = D(dy) act'(pre) without the factor of the elements that stay, which goes into the products' epilogues: where the
 // slope is 0 or 1 dz is then exact in any type.  And the sum of every column over a block of rows.
 // One lane: eight columns (one call of the generator) and every eighth row of the block.
-constexpr int kDzRows = 64;
-
 template <bool BF>
 __global__ __launch_bounds__(kBlock) void k_dz(const void* dy, int64_t dy_ld, const void* pre, int64_t pre_ld, int act, DropArgs drop,
                                                void* dz, int64_t dz_ld, float* partial, int64_t T, int64_t n) {
@@ -33,7 +31,7 @@ __global__ __launch_bounds__(kBlock) void k_dz(const void* dy, int64_t dy_ld, co
     const int lane_c = threadIdx.x & 31, lane_t = threadIdx.x >> 5;
     const int64_t blocks_c = (n + 255) / 256, bt = blockIdx.x / blocks_c, bc = blockIdx.x - bt * blocks_c;
     const int64_t c0 = bc * 256 + 8 * lane_c;
-    const int64_t t0 = bt * kDzRows, t1 = t0 + kDzRows < T ? t0 + kDzRows : T;
+    const int64_t t0 = bt * kSumRows, t1 = t0 + kSumRows < T ? t0 + kSumRows : T;
     const int count = n - c0 < 8 ? (int)(n - c0) : 8;
     Draw d{};
     if (drop.below) d = make_draw(drop.rng, drop.offset);
@@ -52,13 +50,10 @@ __global__ __launch_bounds__(kBlock) void k_dz(const void* dy, int64_t dy_ld, co
 #pragma unroll
                 for (int j = 0; j < 8; ++j) v[j] = dropped(r, j, drop.below) ? 0.f : v[j];
             }
-            if (dz) {   // up to the end of its rows: zero behind the last column
-                if (count < 8)
+            if (count < 8)   // up to the end of its rows: zero behind the last column
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) v[j] = j < count ? v[j] : 0.f;
-                const int to = dz_ld - c0 < 8 ? (int)(dz_ld - c0) : 8;
-                st_oct<BF>(dz, t * dz_ld + c0, to, v);
-            }
+                for (int j = 0; j < 8; ++j) v[j] = j < count ? v[j] : 0.f;
+            st_oct<BF>(dz, t * dz_ld + c0, dz_ld - c0 < 8 ? (int)(dz_ld - c0) : 8, v);
 #pragma unroll
             for (int j = 0; j < 8; ++j) s[j] += v[j];
         }
@@ -103,7 +98,7 @@ Parts parts_of(const LinearCall& c) {
     p.w = c.bf16 && (!c.param_bf16 || c.k % 8) ? take(c.n * p.k_ld * z) : -1;
     p.x = c.bf16 ? take(c.T * p.k_ld * z) : 0;
     p.dz = take(c.T * p.n_ld * z);
-    p.db = take(up(c.T, kDzRows) / kDzRows * c.n * 4);
+    p.db = take(up(c.T, kSumRows) / kSumRows * c.n * 4);
     p.partial = at;
     return p;
 }
@@ -192,7 +187,7 @@ psgd_status launch_linear_backward(const LinearCall& c, std::string* what) {
     const float scale = c.drop.below ? c.drop.factor : 1.f;
     if (c.T == 0 && c.accumulate) return PSGD_OK;
     char* const ws = static_cast<char*>(c.workspace);
-    const int64_t blocks = up(c.T, kDzRows) / kDzRows;
+    const int64_t blocks = up(c.T, kSumRows) / kSumRows;
     const void* dz = c.dy;
     int64_t dz_ld = c.dy_ld;
     bool dz_ready = false;
@@ -203,15 +198,15 @@ psgd_status launch_linear_backward(const LinearCall& c, std::string* what) {
             dz_ld = p.n_ld;
         }
         dz_ready = !direct || (vec_aligned(c.dy, c.dy_ld) && c.n % 8 == 0);
-        if (!direct || c.db) {
+        if (!direct) {
             auto k = c.bf16 ? k_dz<true> : k_dz<false>;
             if ((c.n + 255) / 256 * blocks > 0x7fffffffLL) return PSGD_EUNSUPPORTED;
             hipLaunchKernelGGL(k, dim3((unsigned)((c.n + 255) / 256 * blocks)), dim3(kBlock), 0, s, c.dy, c.dy_ld, c.pre, c.pre_ld, c.act, drop_of(c.drop),
-                               direct ? nullptr : const_cast<void*>(dz), dz_ld, c.db ? reinterpret_cast<float*>(ws + p.db) : nullptr, c.T, c.n);
+                               const_cast<void*>(dz), dz_ld, c.db ? reinterpret_cast<float*>(ws + p.db) : nullptr, c.T, c.n);
             if (failed("k_dz", what)) return PSGD_EHIP;
         }
     }
-    const ColumnSums sums{reinterpret_cast<const float*>(ws + p.db), blocks, c.n, scale, c.db, (int)c.accumulate};
+    const ColumnSums sums{dz == c.dy ? c.dy : nullptr, c.dy_ld, c.T, c.n, reinterpret_cast<float*>(ws + p.db), scale, c.db, (int)c.accumulate};
     ProductCall x{};
     x.bf16 = c.bf16;
     x.ep.scale = scale;
@@ -243,7 +238,7 @@ psgd_status launch_linear_backward(const LinearCall& c, std::string* what) {
             w.ep.residual_ld = c.k;
         }
     }
-    return launch_backward_products(want_x ? &x : nullptr, c.dw ? &w : nullptr, c.db ? &sums : nullptr, what);
+    return launch_backward_products(c.bf16, want_x ? &x : nullptr, c.dw ? &w : nullptr, c.db ? &sums : nullptr, s, what);
 }
 
 }  // namespace psgd

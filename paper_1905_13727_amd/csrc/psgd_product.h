@@ -48,17 +48,21 @@ struct ProductCall {
 int64_t product_partial_bytes(bool bf16, int64_t M, int64_t N, int64_t K);
 psgd_status launch_product(const ProductCall& c, std::string* what);
 
-// The sums of the columns over blocks of rows, [count][n], to be added up and written (or added) to db
+// The bias gradient: sums of the columns over blocks of kSumRows rows, [ceil(T / kSumRows)][n], added up and written (or added) to db.
+// With `dy` the blocks' sums are of that array and still to be computed, otherwise `sums` holds them.
+constexpr int kSumRows = 64;
 struct ColumnSums {
-    const float* sums;
-    int64_t count, n;
+    const void* dy;
+    int64_t dy_ld, T, n;
+    float* sums;
     float scale;
     void* db;
     int accumulate;
 };
 // The input gradient (A along, B across) and the weight gradient (both across) of a layer, each may be null, and its bias gradient.
 // x and w have scratch of their own.
-psgd_status launch_backward_products(const ProductCall* x, const ProductCall* w, const ColumnSums* sums, std::string* what);
+psgd_status launch_backward_products(bool bf16, const ProductCall* x, const ProductCall* w, const ColumnSums* sums, hipStream_t stream,
+                                     std::string* what);
 
 // The forward product of at most kFewTokens tokens, without scratch and whatever the operands' types and alignment
 constexpr int64_t kFewTokens = 32;

@@ -420,13 +420,51 @@ __global__ __launch_bounds__(WM* WN* kWave, 2) void k_product(ProductArgs p) {
     product_tile<BF, AA, BA, AS, BS, WM, WN, MF, NF>(p, blockIdx.x, lds_raw);
 }
 
-// The input gradient (`first` workgroups) and the weight gradient of a layer in one launch: neither waits for the other, and small
-// ones fill the chip together
+// The columns' sums over one block of rows and 256 columns; 256 lanes, each eight columns of every eighth row
+template <bool BF>
+__device__ __forceinline__ void sum_block(const ColumnSums& s, unsigned block, char* lds_raw) {
+    float(*part)[264] = reinterpret_cast<float(*)[264]>(lds_raw);
+    const int lane_c = threadIdx.x & 31, lane_t = threadIdx.x >> 5;
+    const int64_t wide = (s.n + 255) / 256, bt = block / wide, bc = block - bt * wide, c0 = bc * 256 + 8 * lane_c;
+    const int64_t t0 = bt * kSumRows + lane_t;
+    const int count = s.n - c0 < 8 ? (int)(s.n - c0) : 8;
+    float v[8] = {};
+    if (count > 0)
+#pragma unroll
+        for (int r = 0; r < kSumRows; r += 8)
+            if (t0 + r < s.T) {
+                float x[8];
+                ld_oct<BF>(s.dy, (t0 + r) * s.dy_ld + c0, count, x);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] += x[e];
+            }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) part[lane_t][8 * lane_c + e] = v[e];
+    __syncthreads();
+    const int64_t col = bc * 256 + threadIdx.x;
+    if (col >= s.n) return;
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sum += part[i][threadIdx.x];
+    s.sums[bt * s.n + col] = sum;
+}
+
+template <bool BF>
+__global__ __launch_bounds__(256) void k_sum_blocks(ColumnSums s) {
+    __shared__ __attribute__((aligned(16))) char lds_raw[8 * 264 * 4];
+    sum_block<BF>(s, blockIdx.x, lds_raw);
+}
+
+// The input gradient (`first` workgroups) and the weight gradient (up to `second`) of a layer in one launch, and behind them the columns'
+// sums: none waits for another, and small ones fill the chip together
 template <bool BF, Source AS, Source BS, Source BS2, int WM, int WN, int MF, int NF>
-__global__ __launch_bounds__(WM* WN* kWave, 2) void k_product_two(ProductArgs p, ProductArgs q, unsigned first) {
+__global__ __launch_bounds__(WM* WN* kWave, 2) void k_product_two(ProductArgs p, ProductArgs q, ColumnSums sums, unsigned first,
+                                                                  unsigned second) {
     extern __shared__ __attribute__((aligned(16))) char lds_raw[];
+    static_assert(WM * WN * kWave == 256 && Shape<BF, true, false, AS, BS, WM, WN, MF, NF>::kLds >= 8 * 264 * 4, "sum_block");
     if (blockIdx.x < first) product_tile<BF, true, false, AS, BS, WM, WN, MF, NF>(p, blockIdx.x, lds_raw);
-    else product_tile<BF, false, false, AS, BS2, WM, WN, MF, NF>(q, blockIdx.x - first, lds_raw);
+    else if (blockIdx.x < second) product_tile<BF, false, false, AS, BS2, WM, WN, MF, NF>(q, blockIdx.x - first, lds_raw);
+    else sum_block<BF>(sums, blockIdx.x - second, lds_raw);
 }
 
 // The sum over the splits, in order, and the epilogue.  One lane: eight columns.
@@ -459,13 +497,13 @@ template <bool BF>
 __device__ __forceinline__ void column_sums(const ColumnSums& s, int64_t block) {
     __shared__ float part[4][16];
     const int lc = threadIdx.x & 15, lg = threadIdx.x >> 4;
-    const int64_t col = block * 16 + lc;
+    const int64_t col = block * 16 + lc, blocks = (s.T + kSumRows - 1) / kSumRows;
     float v = 0.f;
     if (col < s.n)
-        for (int64_t i = lg; i < s.count; i += 32) {
+        for (int64_t i = lg; i < blocks; i += 32) {
             float x[8];
 #pragma unroll
-            for (int q = 0; q < 8; ++q) x[q] = i + 4 * q < s.count ? s.sums[(i + 4 * q) * s.n + col] : 0.f;
+            for (int q = 0; q < 8; ++q) x[q] = i + 4 * q < blocks ? s.sums[(i + 4 * q) * s.n + col] : 0.f;
 #pragma unroll
             for (int q = 0; q < 8; ++q) v += x[q];
         }
@@ -590,14 +628,17 @@ hipError_t start_by_shape(const ProductCall& p, const Choice& ch) {
     else return by_side(std::false_type(), std::false_type());
 }
 
+// Workgroups of the columns' sums that are still to be computed
+int64_t sum_blocks(const ColumnSums* s) { return s && s->dy ? (s->n + 255) / 256 * ((s->T + kSumRows - 1) / kSumRows) : 0; }
+
 template <bool BF, Source AS, Source BS, Source BS2>
-hipError_t start_two(const ProductArgs& p, const ProductArgs& q, int kind, hipStream_t stream) {
+hipError_t start_two(const ProductArgs& p, const ProductArgs& q, const ColumnSums* sums, int kind, hipStream_t stream) {
     auto go = [&](auto k, auto shape) {
         typedef decltype(shape) S;
-        const unsigned first = (unsigned)(p.tiles_m * p.tiles_n * p.splits);
+        const unsigned first = (unsigned)(p.tiles_m * p.tiles_n * p.splits), second = first + (unsigned)(q.tiles_m * q.tiles_n * q.splits);
         const hipError_t e = with_lds(k, S::kLds);
         if (e != hipSuccess) return e;
-        hipLaunchKernelGGL(k, dim3(first + (unsigned)(q.tiles_m * q.tiles_n * q.splits)), dim3(S::T), S::kLds, stream, p, q, first);
+        hipLaunchKernelGGL(k, dim3(second + (unsigned)sum_blocks(sums)), dim3(S::T), S::kLds, stream, p, q, sums ? *sums : ColumnSums{}, first, second);
         return hipGetLastError();
     };
     return kind == 1 ? go(k_product_two<BF, AS, BS, BS2, 2, 2, 4, 4>, Shape<BF, true, false, AS, BS, 2, 2, 4, 4>())
@@ -666,37 +707,44 @@ psgd_status launch_product(const ProductCall& p, std::string* what) {
     return st != PSGD_OK ? st : join(p.bf16, args_of(p, ch), ProductArgs{}, nullptr, p.stream, what);
 }
 
-psgd_status launch_backward_products(const ProductCall* x, const ProductCall* w, const ColumnSums* sums, std::string* what) {
+psgd_status launch_backward_products(bool bf16, const ProductCall* x, const ProductCall* w, const ColumnSums* sums, hipStream_t stream,
+                                     std::string* what) {
     if (x && w) {
         // In one launch where both take the same tiles and neither has rows or columns over: worth a tile that is not each one's best
         // if what that costs is less than the launch.
         const bool sx = is_straight(*x), sw = is_straight(*w);
-        Choice cx = choose(x->bf16, sx, x->M, x->N, x->K), cw = choose(w->bf16, sw, w->M, w->N, w->K);
+        Choice cx = choose(bf16, sx, x->M, x->N, x->K), cw = choose(bf16, sw, w->M, w->N, w->K);
         if (cx.us + cw.us < 150 && (cx.kind != cw.kind || cx.kind == 0)) {
             double least = cx.us + cw.us + 4;
             for (int kind : {1, 2}) {
-                const Choice tx = choose(x->bf16, sx, x->M, x->N, x->K, kind), tw = choose(w->bf16, sw, w->M, w->N, w->K, kind);
+                const Choice tx = choose(bf16, sx, x->M, x->N, x->K, kind), tw = choose(bf16, sw, w->M, w->N, w->K, kind);
                 if (tx.us + tw.us < least) least = tx.us + tw.us, cx = tx, cw = tw;
             }
         }
-        const int64_t blocks = cx.tiles_m * cx.tiles_n * cx.splits + cw.tiles_m * cw.tiles_n * cw.splits;
+        const int64_t blocks = cx.tiles_m * cx.tiles_n * cx.splits + cw.tiles_m * cw.tiles_n * cw.splits + sum_blocks(sums);
         if (cx.kind == cw.kind && cx.kind > 0 && cx.us + cw.us < 150 && blocks < 0x7fffffffLL) {
             const ProductArgs p = args_of(*x, cx), q = args_of(*w, cw);
-            const hipError_t e = !x->bf16 ? start_two<false, kFp32, kFp32, kFp32>(p, q, cx.kind, x->stream)
-                                 : sx && sw ? start_two<true, kStraight, kStraight, kStraight>(p, q, cx.kind, x->stream)
-                                 : x->b_fp32 ? start_two<true, kBf16, kFp32, kBf16>(p, q, cx.kind, x->stream)
-                                             : start_two<true, kBf16, kBf16, kBf16>(p, q, cx.kind, x->stream);
+            const hipError_t e = !bf16 ? start_two<false, kFp32, kFp32, kFp32>(p, q, sums, cx.kind, stream)
+                                 : sx && sw ? start_two<true, kStraight, kStraight, kStraight>(p, q, sums, cx.kind, stream)
+                                 : x->b_fp32 ? start_two<true, kBf16, kFp32, kBf16>(p, q, sums, cx.kind, stream)
+                                             : start_two<true, kBf16, kBf16, kBf16>(p, q, sums, cx.kind, stream);
             const psgd_status st = product_failed(e, what);
-            return st != PSGD_OK ? st : join(x->bf16, p, q, sums, x->stream, what);
+            return st != PSGD_OK ? st : join(bf16, p, q, sums, stream, what);
         }
+    }
+    if (const int64_t blocks = sum_blocks(sums)) {
+        if (blocks > 0x7fffffffLL) return PSGD_EUNSUPPORTED;
+        auto k = bf16 ? k_sum_blocks<true> : k_sum_blocks<false>;
+        hipLaunchKernelGGL(k, dim3((unsigned)blocks), dim3(256), 0, stream, *sums);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) { *what = std::string("launch k_sum_blocks: ") + hipGetErrorString(e); return PSGD_EHIP; }
     }
     for (const ProductCall* p : {x, w})
         if (p) {
             const psgd_status st = launch_product(*p, what);
             if (st != PSGD_OK) return st;
         }
-    const ProductCall* any = x ? x : w;
-    return sums ? join(any->bf16, ProductArgs{}, ProductArgs{}, sums, any->stream, what) : PSGD_OK;
+    return sums ? join(bf16, ProductArgs{}, ProductArgs{}, sums, stream, what) : PSGD_OK;
 }
 
 }  // namespace psgd
