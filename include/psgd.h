@@ -346,6 +346,7 @@ PSGD_API psgd_status psgd_plan_kept(const psgd_plan* plan, int32_t tensor, int64
  * synchronisation (psgd_random_mask_step: after the plan's first GPU call), so they can be captured and replayed.
  * Buffers are on the current device.  Strides are in elements between consecutive rows; 0 means packed rows. */
 
+/* At infinities they and their slopes take their limits; NaN stays NaN (the slope of RELU at NaN is 0). */
 typedef enum {
     PSGD_ACT_IDENTITY = 0,
     PSGD_ACT_RELU = 1,        /* max(z, 0); slope 0 at 0 */
@@ -370,7 +371,7 @@ typedef struct {
 } psgd_linear;
 
 /* Scratch that psgd_linear_forward and psgd_linear_backward need for this layer and token count (the larger of the
- * two; rng, drop and offset do not matter). */
+ * two; rng, drop and offset do not matter).  It does not shrink as tokens grow: that of the longest batch serves all. */
 PSGD_API psgd_status psgd_linear_workspace(const psgd_plan* plan, const psgd_linear* op, int64_t* bytes);
 
 /* z = x W^T + b ; y = residual + D(act(z)).  x, residual, pre and y have the plan's grad_dtype.

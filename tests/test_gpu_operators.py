@@ -292,6 +292,91 @@ def test_everything_dropped_and_infinities(T, n, k, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("act", B.ACTIVATIONS)
+def test_activations_far_out(act, dtype):
+    """Values and slopes at infinities, far beyond overflow of their squares, and at NaN: their limits, and NaN.  The identity as weights
+    hands each value to its own output."""
+    dev = _need_gpu()
+    n = 40
+    L = Layer(n, n, dtype, dtype, dev, bias=False)
+    L.param[L.w_at:L.w_at + n * n] = torch.eye(n, device=dev).to(DT[dtype]).view(-1)
+    far = torch.tensor([float("inf"), 3e38, 1e20, 1000.0, 100.0, -100.0, -1000.0, -1e20, -3e38, float("-inf")]).to(DT[dtype]).to(dev)
+    for T in (10, 80):   # both products
+        x = torch.zeros(T, n, dtype=DT[dtype], device=dev)
+        x[:10, 3] = torch.where(torch.isinf(far), torch.zeros_like(far), far)   # an infinity times the other weights' zero is NaN
+        y, pre = torch.empty_like(x), torch.empty_like(x)
+        L.plan.linear_forward(1, T, L.param, x, y, L.workspace(T), pre=pre, activation=act, **L.op())
+        assert torch.equal(pre, x)
+        v = x[:10, 3].double()
+        want = v if act == "identity" else v.clamp(min=0)
+        assert bool(((y[:10, 3].double() - want).abs() <= U[dtype] * want.abs() + 1e-6).all()), y[:10, 3]
+        pre[:10, 3] = far
+        pre[:, 5] = float("nan")
+        dy = torch.zeros_like(x)
+        dy[:, 3] = 1.0
+        dy[:, 5] = 1.0
+        dx = torch.empty_like(x)
+        L.plan.linear_backward(1, T, L.param, x, dy, dx, None, L.workspace(T), pre=pre, activation=act, **L.op())
+        slope = torch.ones(10, dtype=torch.float64, device=dev) if act == "identity" else (far.double() > 0).double()
+        if act in ("identity", "relu"):
+            assert bool(torch.isfinite(dx).all()) and torch.equal(dx[:10, 3].double(), slope)
+        else:   # the NaN of column five reaches every output of its row (it meets the other weights' zeros)
+            assert bool(torch.isnan(dx).all())
+            dy[:, 5] = 0.0
+            pre[:, 5] = 0.0
+            L.plan.linear_backward(1, T, L.param, x, dy, dx, None, L.workspace(T), pre=pre, activation=act, **L.op())
+            assert bool(((dx[:10, 3].double() - slope).abs() <= 1e-6).all()), dx[:10, 3]
+
+
+def test_activations_at_infinities():
+    """One input feature: z = x, the infinities reach the activations."""
+    dev = _need_gpu()
+    plan = B.Plan([(8, 2)], 1, 1)
+    param = torch.zeros(plan.sizes.out_elems, device=dev)
+    param[0:16:2] = 1.0
+    for T in (3, 100):
+        x = torch.zeros(T, 2, device=dev)
+        param[1:16:2] = 1.0   # two equal features: infinities of one sign add up
+        x[0], x[1], x[2] = float("inf"), float("-inf"), float("nan")
+        ws = torch.empty(max(1, plan.linear_workspace(0, T)), dtype=torch.uint8, device=dev)
+        for act in B.ACTIVATIONS:
+            y = torch.empty(T, 8, device=dev)
+            plan.linear_forward(0, T, param, x, y, ws, activation=act, stream=_stream())
+            assert bool(torch.isposinf(y[0]).all()) and bool(torch.isnan(y[2]).all()), act
+            assert bool((y[1] == (float("-inf") if act == "identity" else 0.0)).all()), act
+
+
+@pytest.mark.parametrize("T,n,k", [(600, 2304, 520), (2048, 2176, 136)])
+def test_large_layers_in_a_graph(T, n, k):
+    """Forward and backward through the largest tiles, captured and replayed three times with eager work between."""
+    dev = _need_gpu()
+    L = Layer(n, k, "bf16", "f32", dev)
+    x, dy, ws, rng = L.normal(T, k), L.normal(T, n), L.workspace(T), _rng(dev)
+    new = lambda c: torch.zeros(T, c, dtype=torch.bfloat16, device=dev)  # noqa: E731
+
+    def run(y, pre, dx, grad):
+        L.plan.linear_forward(1, T, L.param, x, y, ws, pre=pre, activation="silu", drop=0.25, rng=rng, **L.op())
+        L.plan.linear_backward(1, T, L.param, x, dy, dx, grad, ws, pre=pre, activation="silu", drop=0.25, rng=rng, worker=1, **L.op())
+
+    a, b = [[new(n), new(n), new(k), torch.zeros(2, L.plan.sizes.grad_stride, dtype=torch.bfloat16, device=dev)] for _ in range(2)]
+    run(*a)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        L_op = L.op
+        L.op = lambda **m: dict(L_op(**m), stream=torch.cuda.current_stream().cuda_stream)
+        run(*b)
+    for step in range(3):
+        rng[1] = OFFSET + step
+        x.copy_(L.normal(T, k))
+        run(*a)
+        g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(u, v) for u, v in zip(a, b))
+        assert bool(torch.isfinite(a[3]).all()) and float(a[3].abs().max()) > 0
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("T,n,k", [(1, 640, 2048), (12, 512, 4096), (40, 128, 1024), (600, 520, 264)])
 def test_repeats_bit_for_bit(T, n, k, dtype):
     dev = _need_gpu()
@@ -307,6 +392,22 @@ def test_repeats_bit_for_bit(T, n, k, dtype):
         seen.append((y, dx, grad))
     for other in seen[1:]:
         assert all(torch.equal(a, b) for a, b in zip(seen[0], other))
+
+
+@pytest.mark.parametrize("dtype,params", TYPES)
+@pytest.mark.parametrize("T,n,k", [(1, 96, 4096), (40, 128, 4096), (70, 33, 1001), (700, 260, 130), (300, 1031, 520), (2100, 700, 264), (130, 64, 9000)])
+def test_workspace_is_enough_and_the_longest_batchs_serves_all(T, n, k, dtype, params):
+    dev = _need_gpu()
+    L = Layer(n, k, dtype, params, dev)
+    sizes = [L.plan.linear_workspace(1, t, CODE[params]) for t in range(1, T + 1, max(1, T // 50))] + [L.plan.linear_workspace(1, T, CODE[params])]
+    assert sizes == sorted(sizes)
+    ws = torch.full((sizes[-1] + 8192,), 0xA5, dtype=torch.uint8, device=dev)
+    x, dy, pre = L.normal(T, k), L.normal(T, n), L.normal(T, n)
+    y, dx, grad = torch.empty_like(dy), torch.empty_like(x), torch.zeros(2, L.plan.sizes.grad_stride, dtype=DT[dtype], device=dev)
+    L.plan.linear_forward(1, T, L.param, x, y, ws, activation="silu", **L.op())
+    L.plan.linear_backward(1, T, L.param, x, dy, dx, grad, ws, pre=pre, activation="silu", drop=0.1, rng=_rng(dev), **L.op())
+    L.plan.linear_backward(1, T, L.param, x, dy, dx, grad, ws, **L.op())
+    assert bool((ws[sizes[-1]:] == 0xA5).all())
 
 
 def test_rows_do_not_depend_on_the_others_mask():
