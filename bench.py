@@ -75,9 +75,10 @@ def parse():
                          "(psgd_step_update) or as separate elementwise kernels after psgd_step")
     ap.add_argument("--iterations", type=int, default=1,
                     help="subspace iterations per step (psgd_compress, then psgd_iterate, then psgd_decompress)")
-    ap.add_argument("--compressor", choices=["powersgd", "random_block", "random_k"], default="powersgd",
-                    help="powersgd (the headline), or one of the linear baselines of Appendix G run in the same "
-                         "error-feedback loop (their random draws are made before the timed region)")
+    ap.add_argument("--compressor", choices=["powersgd", "random_block", "random_k", "random_mask"], default="powersgd",
+                    help="powersgd (the headline), one of the linear baselines of Appendix G run in the same "
+                         "error-feedback loop (their random draws are made before the timed region), or the random "
+                         "mask in that loop, whose draw the step makes itself")
     ap.add_argument("--no-cpu-baseline", action="store_true")
     ap.add_argument("--cpu-seconds", type=float, default=15.0, help="budget of the oracle timing")
     ap.add_argument("--tune", action="append", default=[], help="key=value planner tuning (experiments)")
@@ -134,6 +135,7 @@ def byte_models(s, W, gsz, osz, mean, fused_update=False, iterations=1, one_swee
         "k_resident": int(s.bytes_min),                           # read g, e; write e', Delta': each once
         "k_ef_add_zero": int(s.bytes_min),                        # baselines: read g, e; write M; write Delta' = 0 once
         "k_kept_entries": int(s.kept_elems) * (W * 8 + 8),        # read, write M at the kept entries; Delta', values
+        "k_random_mask": int(s.bytes_min),                        # read g, e; write e', Delta': each once
     }
     if fused_update:      # Delta' is not stored; momentum and parameters are read and written instead
         extra = (payload_mat + L) * (16 - osz)
@@ -205,7 +207,9 @@ def cpu_baseline(wl, rank, workers, budget_s, compressor="powersgd"):
 
 
 def cpu_baseline_sparse(wl, rank, workers, budget_s, compressor):
-    """The oracle's Random Block / Random K step on the same workload (numpy fp64; the draws are not timed)."""
+    """The oracle's Random Block / Random K / random mask step on the same workload (numpy fp64; the draws of the first
+    two are not timed, the random mask's is part of its step)."""
+    from oracle import operators_oracle as OO
     from oracle import powersgd_oracle as O
     from paper_1905_13727_amd import workloads as WL
     factors = WL.planted_factors(wl, 0)
@@ -214,9 +218,15 @@ def cpu_baseline_sparse(wl, rank, workers, budget_s, compressor):
     n_elems = sum(int(np.prod(s)) for s in wl.shapes)
     steps, spent = 0, 0.0
     while True:
-        draw = WL.block_starts(wl, rank, 0, steps) if compressor == "random_block" else WL.random_indices(wl, rank, 0, steps)
-        t0 = time.perf_counter()
-        res = (O.random_block_step if compressor == "random_block" else O.random_k_step)(grads, errs, draw, rank)
+        if compressor == "random_mask":
+            t0 = time.perf_counter()
+            keeps = [None if len(s) == 1 else OO.mask_keep(s[0], s[1], t, -1.0, WL.kept_count(s, rank), 7, steps)
+                     for t, s in enumerate(wl.shapes)]
+            res = dict(zip(("out", "err"), OO.random_mask_step(grads, errs, keeps)))
+        else:
+            draw = WL.block_starts(wl, rank, 0, steps) if compressor == "random_block" else WL.random_indices(wl, rank, 0, steps)
+            t0 = time.perf_counter()
+            res = (O.random_block_step if compressor == "random_block" else O.random_k_step)(grads, errs, draw, rank)
         spent += time.perf_counter() - t0
         errs = res["err"]
         steps += 1
@@ -225,7 +235,8 @@ def cpu_baseline_sparse(wl, rank, workers, budget_s, compressor):
     return {"value": round(workers * n_elems * 4 / (spent / steps) / 1e9, 4), "unit": "GB/s", "cores": 1, "kind": "oracle",
             "ms_per_step": round(1e3 * spent / steps, 3),
             "sample": "%d full %s steps of the %s workload (W=%d, r=%d), numpy fp64 elementwise (one thread), same "
-                      "gradient each step, draws not timed" % (steps, compressor, wl.name, workers, rank)}
+                      "gradient each step%s" % (steps, compressor, wl.name, workers, rank,
+                                                "" if compressor == "random_mask" else ", draws not timed")}
 
 
 def main():
@@ -277,7 +288,14 @@ def main():
             return 2
 
     sparse = args.compressor != "powersgd"
-    if sparse:
+    masked = args.compressor == "random_mask"
+    if masked:
+        if args.update != "none" or args.iterations != 1:
+            print("bench.py: the random mask runs without fused update or iterations", file=sys.stderr)
+            return 2
+        # seed and offset of the generator, on the device; every step adds its own number to the offset
+        rng = torch.tensor([7, 0], dtype=torch.int64, device=dev)
+    elif sparse:
         if gdt != "f32" or odt != "f32" or args.update != "none" or args.iterations != 1:
             print("bench.py: the baselines run in fp32, without fused update or iterations", file=sys.stderr)
             return 2
@@ -301,6 +319,9 @@ def main():
                 draws.append(ix)
 
     def step(i):
+        if masked:
+            plan.random_mask_step(grads[i % len(grads)], err, -1.0, rng, out, i, sh)
+            return
         if sparse:
             if args.compressor == "random_block":
                 plan.random_block_step(grads[i % len(grads)], err, draws[i % len(draws)], vals, out, sh)
@@ -346,7 +367,7 @@ def main():
 
     # per-kernel durations: HIP events recorded by the library on its own stream
     plan.set_profiling(True)
-    for i in range(args.profile_steps):
+    for i in range(0 if masked else args.profile_steps):
         step(i)
     kms, ksteps = plan.kernel_times()
     plan.set_profiling(False)
@@ -357,7 +378,9 @@ def main():
     if sparse:
         resident = False
     kavg_events = dict(kavg)
-    if resident and args.update != "separate":
+    if masked:          # one launch as well
+        kavg["k_random_mask"] = event_ms_per_step
+    elif resident and args.update != "separate":
         kavg = {k: 0.0 for k in kavg}
         kavg["k_resident"] = event_ms_per_step
     elif args.update != "separate" and sum(kavg.values()) > 0:
@@ -401,7 +424,7 @@ def main():
     # the dominant kernel's duration in the cold pass: a resident step is that one kernel; a multi-kernel step
     # gets the per-kernel event pairs again, with the caches flushed before every step
     cold_kavg = None
-    if cold_ms is not None and not (resident and args.update != "separate") and args.profile_steps > 0:
+    if cold_ms is not None and not masked and not (resident and args.update != "separate") and args.profile_steps > 0:
         flush = torch.empty(256 * 1024 * 1024, dtype=torch.float32, device=dev)
         plan.set_profiling(True)
         for i in range(args.cold_steps):
@@ -438,10 +461,11 @@ def main():
                           "traffic / algorithmic bytes applied to this set" % rank)
     if (sparse and dom != "k_ef_add_zero") or (not sparse and dom == "k_ef_add_zero"):
         traffic = None
-    compressor_label = {"powersgd": "PowerSGD", "random_block": "Random Block", "random_k": "Random K"}[args.compressor]
+    compressor_label = {"powersgd": "PowerSGD", "random_block": "Random Block", "random_k": "Random K",
+                        "random_mask": "Random Mask"}[args.compressor]
     if args.update != "none" or args.iterations != 1 or tune or unstored or (one_sweep and dom == "k_ef_right"):
         traffic, traffic_source = None, None   # the counters were taken on the plain step with the planner's own choices
-    if resident and args.update != "separate":
+    if masked or (resident and args.update != "separate"):
         cold_dom_ms = cold_ms["median"] if cold_ms else None
     else:
         cold_dom_ms = cold_kavg[dom] if cold_kavg and cold_kavg.get(dom, 0.0) > 0 else None
@@ -464,7 +488,8 @@ def main():
         "config": {"workload": "%s-shaped gradient set, W=%d simulated worker(s), rank %d, gradients %s, output %s"
                                % (wl.name, W, rank, gdt, odt),
                    "compressor": args.compressor,
-                   "mode": "elementwise sweep + kept entries (two kernels)" if sparse else
+                   "mode": "one elementwise sweep that draws the mask itself (one kernel)" if masked else
+                           "elementwise sweep + kept entries (two kernels)" if sparse else
                            "resident (one kernel, M kept in registers)" if resident else
                            ("matrix cores (one walk that stores no M before the decompression)" if unstored
                             else "matrix cores (one kernel per phase)" if plan.path() == "matrix cores"
