@@ -111,6 +111,14 @@ __global__ __launch_bounds__(kFewWaves* kWave, TF == 1 ? 4 : 2) void k_few_token
     for (int a = 0; a < RF; ++a)
 #pragma unroll
         for (int b = 0; b < TF; ++b) acc[a][b] = v4f{0.f, 0.f, 0.f, 0.f};
+    // the eight columns of one token that this lane finishes
+    static_assert(16 * TF * 2 * RF <= kFewWaves * kWave, "one a lane");
+    const int t = threadIdx.x / (2 * RF), c = 8 * (threadIdx.x % (2 * RF));
+    const int64_t j = r0 + c;
+    const bool finishes = t < T && j < n;
+    const int count = n - j < 8 ? (int)(n - j) : 8;
+    const RawOct bias = finishes ? bias_ahead(ep, j, n) : RawOct(), residual = finishes ? residual_ahead<BF>(ep, t * ep.residual_ld + j, count) : RawOct();
+    const DrawWords words = ep.drop.below ? words_ahead(ep.drop.rng, ep.drop.offset) : DrawWords{0, 0, 0, 0};
     const int whole = (int)(k / 64);
     int s = wave;
     for (; s + (kFewDepth - 1) * kFewWaves < whole; s += kFewDepth * kFewWaves) {
@@ -156,21 +164,18 @@ __global__ __launch_bounds__(kFewWaves* kWave, TF == 1 ? 4 : 2) void k_few_token
 #pragma unroll
         for (int b = 0; b < TF; ++b) *reinterpret_cast<v4f*>(&sums[wave][16 * b + i][16 * a + 4 * g]) = acc[a][b];
     __syncthreads();
-    Draw d{};
-    if (ep.drop.below) d = make_draw(ep.drop.rng, ep.drop.offset);
-    for (int item = threadIdx.x; item < T * 2 * RF; item += kFewWaves * kWave) {
-        const int t = item / (2 * RF), c = 8 * (item % (2 * RF));
-        const int64_t j = r0 + c;
-        if (j >= n) continue;
-        float v[8] = {}, bias[8];
+    const Draw d = make_draw(words);
+    if (finishes) {
+        float v[8] = {}, b[8];
 #pragma unroll
         for (int q = 0; q < kFewWaves; ++q) {
             const v4f lo = *reinterpret_cast<const v4f*>(&sums[q][t][c]), hi = *reinterpret_cast<const v4f*>(&sums[q][t][c + 4]);
 #pragma unroll
             for (int e = 0; e < 4; ++e) { v[e] += lo[e]; v[4 + e] += hi[e]; }
         }
-        bias_oct(ep, j, n, bias);
-        finish_oct<BF>(ep, d, y, t * y_ld + j, t * ep.pre_ld + j, t * ep.residual_ld + j, t, j, n - j < 8 ? (int)(n - j) : 8, v, bias);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) b[e] = widened(bias, e, ep.bias_bf);
+        finish_oct<BF>(ep, d, y, t * y_ld + j, t * ep.pre_ld + j, t, j, count, v, b, residual);
     }
 }
 

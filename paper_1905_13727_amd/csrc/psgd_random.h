@@ -14,15 +14,20 @@ struct Draw {   // key and the upper half of the counter, the same in every lane
 };
 
 // rng: {seed, offset} in device memory, so that a captured graph draws anew once the caller has moved the offset on
-__device__ __forceinline__ Draw make_draw(const uint64_t* __restrict__ rng, uint64_t offset) {
+typedef unsigned DrawWords __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ DrawWords words_ahead(const uint64_t* __restrict__ rng, uint64_t offset) {
     const uint64_t seed = rng[0], at = rng[1] + offset;
+    return DrawWords{(unsigned)seed, (unsigned)(seed >> 32), (unsigned)at, (unsigned)(at >> 32)};
+}
+__device__ __forceinline__ Draw make_draw(const DrawWords& w) {
     Draw d;
-    d.k0 = __builtin_amdgcn_readfirstlane((unsigned)seed);
-    d.k1 = __builtin_amdgcn_readfirstlane((unsigned)(seed >> 32));
-    d.c2 = __builtin_amdgcn_readfirstlane((unsigned)at);
-    d.c3 = __builtin_amdgcn_readfirstlane((unsigned)(at >> 32));
+    d.k0 = __builtin_amdgcn_readfirstlane(w[0]);
+    d.k1 = __builtin_amdgcn_readfirstlane(w[1]);
+    d.c2 = __builtin_amdgcn_readfirstlane(w[2]);
+    d.c3 = __builtin_amdgcn_readfirstlane(w[3]);
     return d;
 }
+__device__ __forceinline__ Draw make_draw(const uint64_t* __restrict__ rng, uint64_t offset) { return make_draw(words_ahead(rng, offset)); }
 
 struct Words {
     unsigned w[4];
