@@ -523,6 +523,16 @@ __global__ __launch_bounds__(WM* WN* kWave, 2) void k_product_two(ProductArgs p,
     else sum_block<BF>(sums, blockIdx.x - second, lds_raw);
 }
 
+// The same in the largest tiles, for large products: `first` workgroups of the one whose tiles take longer, so that the other one's fill
+// the units that they leave
+__global__ __launch_bounds__(512, 2) void k_product_two_large(ProductArgs p, ProductArgs q, unsigned first, int p_first) {
+    extern __shared__ __attribute__((aligned(16))) char lds_raw[];
+    const bool head = blockIdx.x < first;
+    const unsigned block = head ? blockIdx.x : blockIdx.x - first;
+    if (head == (p_first != 0)) product_tile<true, true, false, kStraight, kStraight, 2, 4, 8, 4>(p, block, lds_raw);
+    else product_tile<true, false, false, kStraight, kStraight, 2, 4, 8, 4>(q, block, lds_raw);
+}
+
 // The sum over the splits, in order, and the epilogue.  One lane: eight columns.
 template <bool BF>
 __device__ __forceinline__ void join_octs(const ProductArgs& p, int64_t block) {
@@ -629,25 +639,48 @@ Choice choose(bool bf16, bool straight, int64_t M, int64_t N, int64_t K, int onl
     return best;
 }
 
-// Rows (`rows`) or columns beyond the last full tile, and the expected time, if they are a product of their own; 0 if that is slower
+// Rows (`rows`) or columns beyond the last full tile that are better a product of their own, 0 if none are, and the expected time
 struct Rest {
     int64_t count;
     bool rows;
     double us;
 };
 Rest rest_of(bool bf16, bool straight, int64_t M, int64_t N, int64_t K, double whole_us, bool columns_only) {
-    Rest best{0, false, 0.9 * whole_us};
+    Rest best{0, false, whole_us};
     for (int64_t side : {128, 256})
         for (bool rows : {true, false}) {
             const int64_t all = rows ? M : N, r = all % side;
             if ((rows && columns_only) || r == 0 || r > side / 2 || all < side) continue;
             const int64_t m = rows ? M - r : M, n = rows ? N : N - r;
             double us = choose(bf16, straight, m, n, K).us;
-            if (rows) us = rest_of(bf16, straight, m, n, K, us, true).us / 0.9 < us ? rest_of(bf16, straight, m, n, K, us, true).us : us;
+            if (rows) us = rest_of(bf16, straight, m, n, K, us, true).us;
             us += 2 + choose(bf16, straight, rows ? r : M, rows ? N : r, K).us;
-            if (us < best.us) best = Rest{r, rows, us};
+            if (us < 0.9 * whole_us && us < best.us) best = Rest{r, rows, us};
         }
     return best;
+}
+
+// Expected time of a product as launch_product runs it
+double product_us(bool bf16, bool straight, int64_t M, int64_t N, int64_t K) {
+    const double us = choose(bf16, straight, M, N, K).us;
+    return us > 30 ? rest_of(bf16, straight, M, N, K, us, false).us : us;
+}
+
+// Expected time of two products in the largest tiles in one launch, the one with the longer tiles first: units that are through with theirs
+// (some one round earlier than others) take the other one's in turn
+double two_large_us(const Choice& a, const Choice& b) {
+    const TileKind& t = kTilesBf16[0];
+    const double ta = a.steps_each * t.full + t.ends, tb = b.steps_each * t.full + t.ends;
+    const int64_t na = a.tiles_m * a.tiles_n, late = na % kCUs;
+    int64_t nb = b.tiles_m * b.tiles_n;
+    double late_at = ((na + kCUs - 1) / kCUs) * ta, early_at = (na / kCUs) * ta;
+    const int64_t rounds = std::max<int64_t>(0, nb / kCUs - 2 - (int64_t)(ta / tb));   // of all units
+    late_at += rounds * tb, early_at += rounds * tb, nb -= rounds * kCUs;
+    while (nb > 0) {
+        if (late == 0 || early_at <= late_at) early_at += tb, nb -= kCUs - late;
+        else late_at += tb, nb -= late;
+    }
+    return std::max(late ? late_at : 0, early_at);
 }
 
 ProductArgs args_of(const ProductCall& p, const Choice& ch) {
@@ -716,6 +749,19 @@ psgd_status join(bool bf16, const ProductArgs& p, const ProductArgs& q, const Co
     return PSGD_EHIP;
 }
 
+// The columns' sums in a launch of their own, if they are still to be computed
+psgd_status sum_blocks_alone(bool bf16, const ColumnSums* sums, hipStream_t stream, std::string* what) {
+    const int64_t blocks = sum_blocks(sums);
+    if (!blocks) return PSGD_OK;
+    if (blocks > 0x7fffffffLL) return PSGD_EUNSUPPORTED;
+    auto k = bf16 ? k_sum_blocks<true> : k_sum_blocks<false>;
+    hipLaunchKernelGGL(k, dim3((unsigned)blocks), dim3(256), 0, stream, *sums);
+    const hipError_t e = hipGetLastError();
+    if (e == hipSuccess) return PSGD_OK;
+    *what = std::string("launch k_sum_blocks: ") + hipGetErrorString(e);
+    return PSGD_EHIP;
+}
+
 psgd_status product_failed(hipError_t e, std::string* what) {
     if (e == hipSuccess) return PSGD_OK;
     *what = std::string("launch k_product: ") + hipGetErrorString(e);
@@ -770,6 +816,24 @@ psgd_status launch_backward_products(bool bf16, const ProductCall* x, const Prod
         // In one launch where both take the same tiles and neither has rows or columns over: worth a tile that is not each one's best
         // if what that costs is less than the launch.
         const bool sx = is_straight(*x), sw = is_straight(*w);
+        // Large ones where that is expected to be faster than each by itself: 4096 x 2048 x 8192 and 8192 x 2048 x 4096 bf16
+        if (sx && sw) {
+            const Choice lx = choose(true, true, x->M, x->N, x->K, 0), lw = choose(true, true, w->M, w->N, w->K, 0);
+            const bool x_first = lx.steps_each >= lw.steps_each;
+            const int64_t first = (x_first ? lx : lw).tiles_m * (x_first ? lx : lw).tiles_n, all = lx.tiles_m * lx.tiles_n + lw.tiles_m * lw.tiles_n;
+            const double apart = product_us(true, true, x->M, x->N, x->K) + product_us(true, true, w->M, w->N, w->K);
+            if (apart > 60 && all <= 0x7fffffffLL && two_large_us(x_first ? lx : lw, x_first ? lw : lx) < 0.95 * apart) {
+                if (const psgd_status st = sum_blocks_alone(bf16, sums, stream, what); st != PSGD_OK) return st;
+                typedef Shape<true, true, false, kStraight, kStraight, 2, 4, 8, 4> S;
+                hipError_t e = with_lds(k_product_two_large, S::kLds);
+                if (e == hipSuccess) {
+                    hipLaunchKernelGGL(k_product_two_large, dim3((unsigned)all), dim3(S::T), S::kLds, stream, args_of(*x, lx), args_of(*w, lw), (unsigned)first, (int)x_first);
+                    e = hipGetLastError();
+                }
+                const psgd_status st = product_failed(e, what);
+                return st != PSGD_OK || !sums ? st : join(bf16, ProductArgs{}, ProductArgs{}, sums, stream, what);
+            }
+        }
         Choice cx = choose(bf16, sx, x->M, x->N, x->K), cw = choose(bf16, sw, w->M, w->N, w->K);
         if (cx.us + cw.us < 150 && (cx.kind != cw.kind || cx.kind == 0)) {
             double least = cx.us + cw.us + 4;
@@ -789,13 +853,7 @@ psgd_status launch_backward_products(bool bf16, const ProductCall* x, const Prod
             return st != PSGD_OK ? st : join(bf16, p, q, sums, stream, what);
         }
     }
-    if (const int64_t blocks = sum_blocks(sums)) {
-        if (blocks > 0x7fffffffLL) return PSGD_EUNSUPPORTED;
-        auto k = bf16 ? k_sum_blocks<true> : k_sum_blocks<false>;
-        hipLaunchKernelGGL(k, dim3((unsigned)blocks), dim3(256), 0, stream, *sums);
-        const hipError_t e = hipGetLastError();
-        if (e != hipSuccess) { *what = std::string("launch k_sum_blocks: ") + hipGetErrorString(e); return PSGD_EHIP; }
-    }
+    if (const psgd_status st = sum_blocks_alone(bf16, sums, stream, what); st != PSGD_OK) return st;
     for (const ProductCall* p : {x, w})
         if (p) {
             const psgd_status st = launch_product(*p, what);
