@@ -86,6 +86,8 @@ struct Operand {
     // from the tile's first on, those past the end are never stored, but memory may end there.
     // bf16: a chunk that the row's end cuts (or that lies behind it) is read as the row's last eight elements and shifted into place by
     // store(), so that no lane reads past the end and none reads element by element; `tiny` (a row of fewer than eight): it does.
+    // WHOLE: nothing of the step is cut off, and no row is tiny.
+    template <bool WHOLE>
     static __device__ __forceinline__ void load(const char* base, const unsigned (&off)[kLoads], int64_t ld, int64_t extent, int64_t left,
                                                 bool tiny, v4u (&held)[kLoads * kWords]) {
         if constexpr (SRC == kFp32) {   // what lies behind the end reads as zero
@@ -95,11 +97,11 @@ struct Operand {
             for (int i = 0; i < kLoads; ++i) {
                 int line, c;
                 place(i, line, c);
-                const int at = !ALONG && line >= left ? (int)kOutOfRange : (int)off[i];
+                const int at = !WHOLE && !ALONG && line >= left ? (int)kOutOfRange : (int)off[i];
 #pragma unroll
                 for (int h = 0; h < kWords; ++h) held[i * kWords + h] = __builtin_amdgcn_raw_buffer_load_b128(r, at + 16 * h, 0, 0);
             }
-        } else if (tiny) {
+        } else if (!WHOLE && tiny) {
             const int many = (int)(ALONG ? left : extent < ROWS ? extent : ROWS);
 #pragma unroll
             for (int i = 0; i < kLoads; ++i) {
@@ -117,7 +119,7 @@ struct Operand {
 #pragma unroll
             for (int i = 0; i < kLoads; ++i) {
                 int at = (int)off[i];
-                if (left < kStep) {
+                if (!WHOLE && left < kStep) {
                     int line, c;
                     place(i, line, c);
                     if constexpr (ALONG) at += c * kElems < (int)left - 8 ? 0 : ((int)left - 8 - c * kElems) * 2;
@@ -127,6 +129,7 @@ struct Operand {
             }
         }
     }
+    template <bool WHOLE>
     static __device__ __forceinline__ void store(const v4u (&held)[kLoads * kWords], int64_t extent, int64_t left, bool tiny, lds_char* to) {
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
@@ -134,7 +137,7 @@ struct Operand {
 #pragma unroll
             for (int h = 0; h < kWords; ++h) t[h] = held[i * kWords + h];
             if constexpr (SRC == kFp32) {
-                if (ALONG && left < kStep) {
+                if (!WHOLE && ALONG && left < kStep) {
                     int line, c;
                     place(i, line, c);
 #pragma unroll
@@ -143,7 +146,7 @@ struct Operand {
                         for (int e = 0; e < 4; ++e)
                             if (c * kElems + 4 * h + e >= left) t[h][e] = 0;
                 }
-            } else if (!tiny && ((!ALONG && extent < ROWS) || left < kStep)) {
+            } else if ((WHOLE || !tiny) && ((!ALONG && extent < ROWS) || (!WHOLE && left < kStep))) {
                 int line, c;
                 place(i, line, c);
                 const int many = (int)(ALONG ? left : extent < ROWS ? extent : ROWS);
@@ -307,36 +310,31 @@ __device__ __forceinline__ void product_tile(const ProductArgs& p, unsigned bloc
     // Step s: straight to LDS at once, through registers by settle() one barrier later.  `left` of the contraction from step s on,
     // for the loads through registers.
     v4u a_held[A::kLoads * A::kWords], b_held[B::kLoads * B::kWords];
-    auto fetch = [&](int s, int buf) __attribute__((always_inline)) {
+    auto fetch = [&](auto all, int s, int buf) __attribute__((always_inline)) {
+        constexpr bool W = decltype(all)::value;
         lds_char* to = lds + buf * S::kStepBytes;
         const int64_t left = K - (s0 + s) * A::kStep;
         if constexpr (AS == kStraight) {
-            if (s < whole) A::load(ap, a_off, to);
+            if (W || s < whole) A::load(ap, a_off, to);
             else A::load_cut(ap, a_off, to, cut);
         } else {
-            A::load(ap, a_off, a_ld, M - i0, left, (AA ? K : M) < 8, a_held);
+            A::template load<W>(ap, a_off, a_ld, M - i0, left, (AA ? K : M) < 8, a_held);
         }
         if constexpr (BS == kStraight) {
-            if (s < whole) B::load(bp, b_off, to + A::kBytes);
+            if (W || s < whole) B::load(bp, b_off, to + A::kBytes);
             else B::load_cut(bp, b_off, to + A::kBytes, cut);
         } else {
-            B::load(bp, b_off, b_ld, N - j0, left, (BA ? K : N) < 8, b_held);
+            B::template load<W>(bp, b_off, b_ld, N - j0, left, (BA ? K : N) < 8, b_held);
         }
         ap += A::step_bytes(a_ld);
         bp += B::step_bytes(b_ld);
     };
-    auto fetch_whole = [&](int buf) __attribute__((always_inline)) {
-        lds_char* to = lds + buf * S::kStepBytes;
-        A::load(ap, a_off, to);
-        B::load(bp, b_off, to + A::kBytes);
-        ap += A::step_bytes(a_ld);
-        bp += B::step_bytes(b_ld);
-    };
-    auto settle = [&](int s, int buf) __attribute__((always_inline)) {
+    auto settle = [&](auto all, int s, int buf) __attribute__((always_inline)) {
+        constexpr bool W = decltype(all)::value;
         lds_char* to = lds + buf * S::kStepBytes;
         const int64_t left = K - (s0 + s) * A::kStep;
-        if constexpr (AS != kStraight) A::store(a_held, M - i0, left, (AA ? K : M) < 8, to);
-        if constexpr (BS != kStraight) B::store(b_held, N - j0, left, (BA ? K : N) < 8, to + A::kBytes);
+        if constexpr (AS != kStraight) A::template store<W>(a_held, M - i0, left, (AA ? K : M) < 8, to);
+        if constexpr (BS != kStraight) B::template store<W>(b_held, N - j0, left, (BA ? K : N) < 8, to + A::kBytes);
         __builtin_amdgcn_s_waitcnt(kLandedAndRead);
     };
     auto read = [&](int buf, int h, Frag (&x)[MF], Frag (&y)[NF]) __attribute__((always_inline)) {
@@ -379,31 +377,34 @@ __device__ __forceinline__ void product_tile(const ProductArgs& p, unsigned bloc
     };
     if (steps > 0) {
         Frag x0[MF], y0[NF], x1[MF], y1[NF];
-        fetch(0, 0);
+        const std::true_type all;
+        const std::false_type some;
+        fetch(some, 0, 0);
         ends_ahead();
-        settle(0, 0);
+        settle(some, 0, 0);
         __syncthreads();
-        if (steps > 1) fetch(1, 1);
+        if (steps > 1) fetch(some, 1, 1);
         read(0, 0, x0, y0);
         int buf = 0, s = 0;
-        if constexpr (BF && AS == kStraight && BS == kStraight) {
-            // Steps with two whole ones behind them have no branches, so that their loads and reads of LDS can stand between the products: a wave
-            // goes on multiplying while it asks for what comes next.  4096 x 8192 x 4096 along / along 228 us with the branches, 216 without, 202
-            // dealt out in the order above; 8192 x 2048 x 4096 across / across, with twice the reads, 129, 113 and 116, so there the order is
-            // left to the compiler.
-            for (; s + 2 < whole; ++s, buf ^= 1) {
-                read(buf, 1, x1, y1);
-                multiply(x0, y0);
-                if constexpr (AA && BA) deal_out<0, MF + NF, MF * NF>();
-                __builtin_amdgcn_sched_barrier(0);
-                settle(s + 1, buf ^ 1);
-                __syncthreads();
-                fetch_whole(buf);
-                read(buf ^ 1, 0, x0, y0);
-                multiply(x1, y1);
-                if constexpr (AA && BA) deal_out<A::kLoads + B::kLoads, MF + NF, MF * NF>();
-                __builtin_amdgcn_sched_barrier(0);
-            }
+        // Steps with two whole ones behind them have no branches, so that their loads and reads of LDS can stand between the products: a wave goes
+        // on multiplying while it asks for what comes next.  4096 x 8192 x 4096 along / along 228 us with the branches, 216 without, 202 dealt
+        // out in the order above; 8192 x 2048 x 4096 across / across, with twice the reads, 129, 113 and 116, so there the order is left to the
+        // compiler, as it is where loads go through registers.
+        constexpr bool kDeal = BF && AA && BA && AS == kStraight && BS == kStraight;
+        const int64_t least = std::min(AA ? K : M, BA ? K : N);
+        const int plain = AS == kStraight || BF == false || least >= 8 ? whole : 0;
+        for (; s + 2 < plain; ++s, buf ^= 1) {
+            read(buf, 1, x1, y1);
+            multiply(x0, y0);
+            if constexpr (kDeal) deal_out<0, MF + NF, MF * NF>();
+            __builtin_amdgcn_sched_barrier(0);
+            settle(all, s + 1, buf ^ 1);
+            __syncthreads();
+            fetch(all, s + 2, buf);
+            read(buf ^ 1, 0, x0, y0);
+            multiply(x1, y1);
+            if constexpr (kDeal) deal_out<A::kLoads + B::kLoads, MF + NF, MF * NF>();
+            __builtin_amdgcn_sched_barrier(0);
         }
         for (; s < steps; ++s, buf ^= 1) {
             read(buf, 1, x1, y1);
@@ -411,9 +412,9 @@ __device__ __forceinline__ void product_tile(const ProductArgs& p, unsigned bloc
             multiply(x0, y0);
             __builtin_amdgcn_sched_barrier(0);
             if (s + 1 < steps) {
-                settle(s + 1, buf ^ 1);   // step s + 1 has landed, this step's fragments are in registers
+                settle(some, s + 1, buf ^ 1);   // step s + 1 has landed, this step's fragments are in registers
                 __syncthreads();
-                if (s + 2 < steps) fetch(s + 2, buf);
+                if (s + 2 < steps) fetch(some, s + 2, buf);
                 read(buf ^ 1, 0, x0, y0);
             }
             __builtin_amdgcn_sched_barrier(0);
