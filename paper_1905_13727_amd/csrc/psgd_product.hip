@@ -638,14 +638,20 @@ namespace {
 constexpr int kCUs = 256;
 
 // The tiles, and what they take: us a step with a unit full, of one tile by itself, and for first loads and epilogue; tiles that a
-// unit holds at once.  Measured on products of one to four rounds, 512 .. 16384 of the contraction.
+// unit holds at once.  Fitted to products of one to four rounds, 128 .. 8192 of the contraction; bf16 both operands straight to LDS along
+// the contraction, and all others (reads across it, loads through registers).  Over 39 bf16 products and every division that was timed the
+// choice takes 0.9 % more than the best one on average, 21 % at most (128 x 2048 x 2048, 14.3 and 11.8 us); over 39 fp32 ones 0.8 and 5 %.
 struct TileKind {
     int side;
     int at_once;
     double full, alone, ends;
 };
-constexpr TileKind kTilesBf16[] = {{256, 1, 1.46, 1.46, 10}, {128, 2, 0.47, 0.7, 5}, {64, 4, 0.155, 0.5, 3}};
-constexpr TileKind kTilesFp32[] = {{0, 0, 0, 0, 0}, {128, 2, 1.9, 2.4, 5}, {64, 4, 0.5, 0.8, 3}};
+constexpr TileKind kTilesAlong[] = {{256, 1, 1.2, 1.2, 9}, {128, 2, 0.41, 0.42, 5.7}, {64, 4, 0.138, 0.204, 3.5}};
+constexpr TileKind kTilesAcross[] = {{256, 1, 1.36, 1.36, 8.5}, {128, 2, 0.465, 0.735, 4.4}, {64, 4, 0.163, 0.46, 2.9}};
+constexpr TileKind kTilesFp32[] = {{256, 1, 0, 0, 0}, {128, 2, 1.9, 2.4, 5}, {64, 4, 0.5, 0.8, 3}};   // none of 256
+// How a product's operands come
+enum Way { kInFp32, kByRegisters, kStraightAcross, kStraightAlong };
+const TileKind& tile_kind(Way way, int kind) { return (way == kInFp32 ? kTilesFp32 : way == kStraightAlong ? kTilesAlong : kTilesAcross)[kind]; }
 
 // A split takes four steps at least, and there are no more tiles and splits than the units hold at a time, so that the sums
 // take at most 64 MiB whatever the sizes.
@@ -658,13 +664,13 @@ struct Choice {
 };
 
 // The tile and the division of the contraction with the least expected time: steps of a tile one after the other, as many tiles
-// at a time as the units hold, and the sums of the splits written and read again.  `straight`: both operands go straight to LDS.
-Choice choose(bool bf16, bool straight, int64_t M, int64_t N, int64_t K, int only = -1) {
-    const int64_t steps = (K + (bf16 ? 63 : 31)) / (bf16 ? 64 : 32);
+// at a time as the units hold, and the sums of the splits written and read again.
+Choice choose(Way way, int64_t M, int64_t N, int64_t K, int only = -1) {
+    const int64_t step = way == kInFp32 ? 32 : 64, steps = (K + step - 1) / step;
     Choice best{-1, 0, 0, 0, 0, 0};
     for (int kind = 0; kind < 3; ++kind) {
-        const TileKind& t = bf16 ? kTilesBf16[kind] : kTilesFp32[kind];
-        if (!t.side || (kind == 0 && !straight) || (only >= 0 && kind != only)) continue;
+        const TileKind& t = tile_kind(way, kind);
+        if ((kind == 0 && way < kStraightAcross) || (only >= 0 && kind != only)) continue;
         if (only < 0 && t.side > 64 && (M <= t.side / 2 || N <= t.side / 2)) continue;   // more than half of every tile outside
         const int64_t tm = (M + t.side - 1) / t.side, tn = (N + t.side - 1) / t.side, tiles = tm * tn;
         for (int64_t splits = 1; splits <= (kind == 0 ? 1 : kMostSplits) && (splits == 1 || (splits <= steps / kLeastSteps && tiles * splits <= kCUs * t.at_once)); ++splits) {
@@ -675,7 +681,7 @@ Choice choose(bool bf16, bool straight, int64_t M, int64_t N, int64_t K, int onl
             const double left = rest == 0 ? 0 : std::max<double>((double)((rest + kCUs - 1) / kCUs), batches ? 0.8 * t.at_once : 0);
             const double work = batches * t.at_once + left;
             double us = each * std::max(t.alone, work * t.full) + t.ends * std::max<double>(1, work / std::min(t.at_once, 2));
-            if (splits > 1) us += 4 + 2e-6 * splits * M * N;
+            if (splits > 1) us += 4.2 + 1.6e-6 * splits * M * N;
             if (best.kind < 0 || us < best.us) best = Choice{kind, splits, each, tm, tn, us};
         }
     }
@@ -688,31 +694,31 @@ struct Rest {
     bool rows;
     double us;
 };
-Rest rest_of(bool bf16, bool straight, int64_t M, int64_t N, int64_t K, double whole_us, bool columns_only) {
+Rest rest_of(Way way, int64_t M, int64_t N, int64_t K, double whole_us, bool columns_only) {
     Rest best{0, false, whole_us};
     for (int64_t side : {128, 256})
         for (bool rows : {true, false}) {
             const int64_t all = rows ? M : N, r = all % side;
             if ((rows && columns_only) || r == 0 || r > side / 2 || all < side) continue;
             const int64_t m = rows ? M - r : M, n = rows ? N : N - r;
-            double us = choose(bf16, straight, m, n, K).us;
-            if (rows) us = rest_of(bf16, straight, m, n, K, us, true).us;
-            us += 2 + choose(bf16, straight, rows ? r : M, rows ? N : r, K).us;
+            double us = choose(way, m, n, K).us;
+            if (rows) us = rest_of(way, m, n, K, us, true).us;
+            us += 2 + choose(way, rows ? r : M, rows ? N : r, K).us;
             if (us < 0.9 * whole_us && us < best.us) best = Rest{r, rows, us};
         }
     return best;
 }
 
 // Expected time of a product as launch_product runs it
-double product_us(bool bf16, bool straight, int64_t M, int64_t N, int64_t K) {
-    const double us = choose(bf16, straight, M, N, K).us;
-    return us > 30 ? rest_of(bf16, straight, M, N, K, us, false).us : us;
+double product_us(Way way, int64_t M, int64_t N, int64_t K) {
+    const double us = choose(way, M, N, K).us;
+    return us > 30 ? rest_of(way, M, N, K, us, false).us : us;
 }
 
 // Expected time of two products in the largest tiles in one launch, the one with the longer tiles first: units that are through with theirs
 // (some one round earlier than others) take the other one's in turn
 double two_large_us(const Choice& a, const Choice& b) {
-    const TileKind& t = kTilesBf16[0];
+    const TileKind& t = kTilesAcross[0];
     const double ta = a.steps_each * t.full + t.ends, tb = b.steps_each * t.full + t.ends;
     const int64_t na = a.tiles_m * a.tiles_n, late = na % kCUs;
     int64_t nb = b.tiles_m * b.tiles_n;
@@ -778,7 +784,10 @@ hipError_t start_two(const ProductArgs& p, const ProductArgs& q, const ColumnSum
                      : go(k_product_two<BF, AS, BS, BS2, 2, 2, 2, 2>, Shape<BF, true, false, AS, BS, 2, 2, 2, 2>());
 }
 
-bool is_straight(const ProductCall& p) { return p.bf16 && p.a_ready && p.b_ready && !p.b_fp32; }
+Way way_of(const ProductCall& p) {
+    if (!p.bf16) return kInFp32;
+    return !p.a_ready || !p.b_ready || p.b_fp32 ? kByRegisters : p.a_along && p.b_along ? kStraightAlong : kStraightAcross;
+}
 int64_t join_blocks(const ProductArgs& p) { return p.partial ? (p.M * ((p.N + 7) / 8) + kWave - 1) / kWave : 0; }
 
 psgd_status join(bool bf16, const ProductArgs& p, const ProductArgs& q, const ColumnSums* sums, hipStream_t stream, std::string* what) {
@@ -819,13 +828,13 @@ int64_t product_partial_bytes(bool bf16, int64_t M, int64_t N, int64_t K) {
 }
 
 psgd_status launch_product(const ProductCall& p, std::string* what) {
-    const bool straight = is_straight(p);
-    const Choice ch = choose(p.bf16, straight, p.M, p.N, p.K);
+    const Way way = way_of(p);
+    const Choice ch = choose(way, p.M, p.N, p.K);
     if (ch.tiles_m * ch.tiles_n * ch.splits > 0x7fffffffLL) return PSGD_EUNSUPPORTED;
     // Rows or columns beyond the last full tile cost a row of tiles, which may be the one too many for the last round: a product of
     // their own, in small tiles, where that is expected to be faster by a tenth.  4099 x 2048 x 8192 bf16 205 us in one, 149 in two.
     if (ch.us > 30) {
-        const Rest over = rest_of(p.bf16, straight, p.M, p.N, p.K, ch.us, false);
+        const Rest over = rest_of(way, p.M, p.N, p.K, ch.us, false);
         const int64_t rest = over.count;
         const bool rows = over.rows;
         if (rest) {
@@ -848,7 +857,7 @@ psgd_status launch_product(const ProductCall& p, std::string* what) {
             return launch_product(q, what);
         }
     }
-    const psgd_status st = product_failed(!p.bf16 ? start_by_shape<false, kFp32, kFp32>(p, ch) : straight ? start_by_shape<true, kStraight, kStraight>(p, ch)
+    const psgd_status st = product_failed(!p.bf16 ? start_by_shape<false, kFp32, kFp32>(p, ch) : way >= kStraightAcross ? start_by_shape<true, kStraight, kStraight>(p, ch)
                                           : p.b_fp32 ? start_by_shape<true, kBf16, kFp32>(p, ch) : start_by_shape<true, kBf16, kBf16>(p, ch), what);
     return st != PSGD_OK ? st : join(p.bf16, args_of(p, ch), ProductArgs{}, nullptr, p.stream, what);
 }
@@ -858,13 +867,14 @@ psgd_status launch_backward_products(bool bf16, const ProductCall* x, const Prod
     if (x && w) {
         // In one launch where both take the same tiles and neither has rows or columns over: worth a tile that is not each one's best
         // if what that costs is less than the launch.
-        const bool sx = is_straight(*x), sw = is_straight(*w);
+        const Way vx = way_of(*x), vw = way_of(*w);
+        const bool sx = vx >= kStraightAcross, sw = vw >= kStraightAcross;
         // Large ones where that is expected to be faster than each by itself: 4096 x 2048 x 8192 and 8192 x 2048 x 4096 bf16
         if (sx && sw) {
-            const Choice lx = choose(true, true, x->M, x->N, x->K, 0), lw = choose(true, true, w->M, w->N, w->K, 0);
+            const Choice lx = choose(vx, x->M, x->N, x->K, 0), lw = choose(vw, w->M, w->N, w->K, 0);
             const bool x_first = lx.steps_each >= lw.steps_each;
             const int64_t first = (x_first ? lx : lw).tiles_m * (x_first ? lx : lw).tiles_n, all = lx.tiles_m * lx.tiles_n + lw.tiles_m * lw.tiles_n;
-            const double apart = product_us(true, true, x->M, x->N, x->K) + product_us(true, true, w->M, w->N, w->K);
+            const double apart = product_us(vx, x->M, x->N, x->K) + product_us(vw, w->M, w->N, w->K);
             if (apart > 60 && all <= 0x7fffffffLL && two_large_us(x_first ? lx : lw, x_first ? lw : lx) < 0.95 * apart) {
                 if (const psgd_status st = sum_blocks_alone(bf16, sums, stream, what); st != PSGD_OK) return st;
                 typedef Shape<true, true, false, kStraight, kStraight, 2, 4, 8, 4> S;
@@ -877,11 +887,11 @@ psgd_status launch_backward_products(bool bf16, const ProductCall* x, const Prod
                 return st != PSGD_OK || !sums ? st : join(bf16, ProductArgs{}, ProductArgs{}, sums, stream, what);
             }
         }
-        Choice cx = choose(bf16, sx, x->M, x->N, x->K), cw = choose(bf16, sw, w->M, w->N, w->K);
+        Choice cx = choose(vx, x->M, x->N, x->K), cw = choose(vw, w->M, w->N, w->K);
         if (cx.us + cw.us < 150 && (cx.kind != cw.kind || cx.kind == 0)) {
             double least = cx.us + cw.us + 4;
             for (int kind : {1, 2}) {
-                const Choice tx = choose(bf16, sx, x->M, x->N, x->K, kind), tw = choose(bf16, sw, w->M, w->N, w->K, kind);
+                const Choice tx = choose(vx, x->M, x->N, x->K, kind), tw = choose(vw, w->M, w->N, w->K, kind);
                 if (tx.us + tw.us < least) least = tx.us + tw.us, cx = tx, cw = tw;
             }
         }
