@@ -9,9 +9,11 @@
 namespace psgd {
 
 // y = residual + D(x).  One lane: eight consecutive columns of a row, one call of the generator.  A workgroup: `high` rows of a band of
-// `wide` groups of eight columns, about kDropItems of them; which row an item lies in is a multiplication (recip =
-// ceil(2^32 / wide), 0 for one group; exact below 2^16 items).
-constexpr int kDropItems = 1024;
+// `wide` groups of eight columns, about kDropItems of them, or one a lane where there are too few for every unit; which row an item lies
+// in is a multiplication (recip = ceil(2^32 / wide), 0 for one group; exact below 2^16 items).
+// Memory bounds it, not the generator: 16384 x 2048 bf16 with a residual 39.5 us, 5.1 TB/s; 8191 x 8191 bf16, rows that begin at any element,
+// 55.6 us, 4.8 TB/s.
+constexpr int kDropItems = 1024, kDropFew = 256 * kDropItems;
 
 template <bool BF>
 __global__ __launch_bounds__(kBlock) void k_dropout(const void* x, int64_t x_ld, const void* residual, int64_t residual_ld, void* y,
@@ -19,23 +21,21 @@ __global__ __launch_bounds__(kBlock) void k_dropout(const void* x, int64_t x_ld,
                                                     int64_t bands, DropArgs drop) {
     const int64_t strip = blockIdx.x / bands, g0 = (blockIdx.x - strip * bands) * wide, row0 = strip * high;
     const int n = (int)(rows - row0 < high ? rows - row0 : high) * wide;
-    Draw d{};
-    if (drop.below) d = make_draw(drop.rng, drop.offset);
+    const DrawWords words = drop.below ? words_ahead(drop.rng, drop.offset) : DrawWords{0, 0, 0, 0};   // in flight with the first loads
     for (int item = threadIdx.x; item < n; item += kBlock) {
         const int r = recip ? (int)__umulhi((unsigned)item, recip) : item;
         const int64_t row = row0 + r, col = 8 * (g0 + item - r * wide);
         const int count = (int)(cols - col < 8 ? cols - col : 8);
         if (count <= 0) continue;
-        float v[8];
+        float v[8], z[8];
         ld_oct<BF>(x, row * x_ld + col, count, v);
+        if (residual) ld_oct<BF>(residual, row * residual_ld + col, count, z);
         if (drop.below) {
-            const Words w = philox(d, (unsigned)(col >> 3), (unsigned)row);
+            const Words w = philox(make_draw(words), (unsigned)(col >> 3), (unsigned)row);
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[e] = dropped(w, e, drop.below) ? 0.f : v[e] * drop.factor;
         }
         if (residual) {
-            float z[8];
-            ld_oct<BF>(residual, row * residual_ld + col, count, z);
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[e] += z[e];
         }
@@ -45,8 +45,9 @@ __global__ __launch_bounds__(kBlock) void k_dropout(const void* x, int64_t x_ld,
 
 psgd_status launch_dropout(const DropoutCall& c, std::string* what) {
     const int64_t groups = (c.cols + 7) / 8;
-    const int wide = (int)(groups < kDropItems ? groups : kDropItems);
-    const int high = wide < kDropItems ? kDropItems / wide : 1;
+    const int items = c.rows * groups <= kDropFew ? kBlock : kDropItems;   // 700 x 650 fp32 5.0 us with 1024, 3.5 with 256
+    const int wide = (int)(groups < items ? groups : items);
+    const int high = wide < items ? items / wide : 1;
     const unsigned recip = wide > 1 ? (unsigned)(((uint64_t(1) << 32) + wide - 1) / wide) : 0;
     const int64_t bands = (groups + wide - 1) / wide, blocks = (c.rows + high - 1) / high * bands;
     if (blocks > 0x7fffffffLL) return PSGD_EUNSUPPORTED;
