@@ -180,20 +180,23 @@ __global__ __launch_bounds__(kFewWaves* kWave, TF == 1 ? 4 : 2) void k_few_token
 }
 
 // Where this takes less time than the tiles of the other products, which read x once for 64 rows of W and divide the contraction
-// over the chip: us, this / tiles, one, 16 and 32 tokens.
-//   fp32: 8192 x 2048 (n x k) 16 / 29, 19 / 29, 23 / 30; 50304 x 2048 83 / 153, 107 / 151, 117 / 153; 2048 x 8192, short of workgroups, 23 / 32,
-//   32 / 34, 46 / 34.
-//   bf16: 2048 x 2048 6.9 / 12.1, 8.5 / 12.0, 9.7 / 12.2; 8192 x 2048 9.0 / 12.5, 10.1 / 13.3, 12.2 / 14.5; beyond 2^24 weights it loses: 8192 x
-//   8192 30 / 28, 35 / 28, 48 / 29; 50304 x 2048 41 / 33, 48 / 34, 58 / 35; and where n is small or rows of odd length begin between words:
-//   2048 x 8192 14 / 16, 19 / 17, 26 / 18; 4096 x 4095 21 / 16, 33 / 18, 46 / 18.
-//   bf16, fp32 weights: 1000 x 1001 8.6 / 11.8, 8.7 / 11.9, 11.1 / 12.0; 2048 x 2048 8.7 / 11.6, 11.4 / 12.2, 14.8 / 12.9; 8192 x 2048 16 / 18,
-//   19 / 18, 22 / 18.
+// over the chip: us, this / tiles, one, 16 and 32 tokens, n x k.
+//   fp32: 650 x 650 4.3 / 9.7, 4.6 / 9.8, 6.4 / 10.1; 8192 x 2048 12.9 / 24.9, 16.9 / 25.3, 18.4 / 26.2; 50304 x 2048 82 / 137, 107 / 137, 119 / 138;
+//   2048 x 8192, short of workgroups, 20.5 / 25.9, 30.4 / 26.3, 44.5 / 26.8; 512 x 8192 19.6 / 13.3.
+//   bf16: 512 x 512 2.9 / 4.6, 3.3 / 4.7, 3.7 / 5.0; 2048 x 2048 4.4 / 6.6, 5.8 / 7.0, 7.5 / 7.6; 8192 x 2048 6.6 / 9.9, 7.9 / 16.1, 9.8 / 16.6; beyond
+//   2^24 weights it loses: 8192 x 4096 16.3 / 15.0, 16.4 / 15.7, 17.9 / 16.5; 50304 x 2048 39 / 31, 44 / 32, 52 / 34; and where n is small or
+//   rows of odd length begin between words: 2048 x 8192 11.6 / 10.6, 16.6 / 12.1, 23.6 / 13.0; 1000 x 1001 6.5 / 7.2, 8.7 / 7.9, 11.5 / 8.1; 4096 x
+//   4095 18.7 / 11.5, 30.3 / 13.0, 43.4 / 13.7.
+//   bf16, fp32 weights: 512 x 512 3.4 / 6.0, 4.1 / 6.0, 5.0 / 6.5; 1000 x 1001 4.8 / 7.4, 6.6 / 8.0, 9.4 / 8.2; 2048 x 2048 6.9 / 7.5, 9.5 / 8.0, 13.0 / 8.6;
+//   8192 x 2048 12.5 / 15.1, 16.8 / 15.9, 18.9 / 16.6; 50304 x 2048 69 / 103, 97 / 105, 109 / 108.
 bool few_tokens(const LinearCall& c) {
     if (c.T > kFewTokens) return false;
     const int64_t weights = c.n * c.k;
-    if (!c.bf16) return c.T <= 16 || 2 * c.n >= c.k;
-    if (2 * c.n < c.k || (c.param_bf16 && c.k % 2 && weights > (1 << 21))) return false;
-    return weights <= (c.T <= 16 || c.param_bf16 ? 1 << 24 : 1 << 21);
+    const bool one = c.T <= 4, some = c.T <= 16;
+    if (!c.bf16) return 2 * c.n >= c.k || (one && 4 * c.n >= c.k);
+    if (2 * c.n < c.k) return false;
+    if (!c.param_bf16) return one || weights <= (some ? 1 << 20 : 1 << 19);
+    return c.k % 2 ? one && weights <= 1 << 21 : weights <= 1 << 24;
 }
 
 namespace {
@@ -201,8 +204,8 @@ namespace {
 template <bool BF, bool WBF>
 hipError_t start(const LinearCall& c, const Epilogue& ep) {
     // 32 rows a workgroup where that still is one for every compute unit: x is read from the caches half as often.  8192 x 2048 bf16, 16
-    // and 32 tokens: 10.1 and 12.2 us, with 16 rows 12.0 and 15.7; 4096 x 1024 16 tokens 9.1 and 9.0; fp32 with few tokens loads enough
-    // with 16 (one token 15.6, with 32 rows 20.6)
+    // and 32 tokens: 7.9 and 9.8 us, with 16 rows 9.7 and 13.2; 4096 x 1024, 16 tokens 5.0 and 4.2; fp32 with few tokens loads enough with
+    // 16 (8192 x 2048, one token 12.9, with 32 rows 16.1; 32 tokens 23.8 and 18.4)
     const bool two = c.n >= 32 * 256 && (WBF || c.T > 16);
     const int64_t rows = two ? 32 : 16;
     auto k = two ? (c.T <= 16 ? k_few_tokens<BF, WBF, 2, 1> : k_few_tokens<BF, WBF, 2, 2>) : (c.T <= 16 ? k_few_tokens<BF, WBF, 1, 1> : k_few_tokens<BF, WBF, 1, 2>);

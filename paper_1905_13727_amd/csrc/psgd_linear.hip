@@ -37,25 +37,38 @@ __global__ __launch_bounds__(kBlock) void k_dz(const void* dy, int64_t dy_ld, co
     if (drop.below) d = make_draw(drop.rng, drop.offset);
     float s[8] = {};
     if (count > 0) {
-        for (int64_t t = t0 + lane_t; t < t1; t += 8) {
-            float v[8];
-            ld_oct<BF>(dy, t * dy_ld + c0, count, v);
-            if (act != PSGD_ACT_IDENTITY) {
-                float z[8];
-                ld_oct<BF>(pre, t * pre_ld + c0, count, z);
-                slope_oct(z, v, act);
+        constexpr int kAhead = 4;   // rows asked for at a time, ahead of the stores that a later load would wait for
+        constexpr int z = BF ? 2 : 4;
+        for (int64_t t = t0 + lane_t; t < t1; t += 8 * kAhead) {
+            RawOct a[kAhead], b[kAhead];
+#pragma unroll
+            for (int q = 0; q < kAhead; ++q)
+                if (t + 8 * q < t1) {
+                    a[q] = ld_raw(static_cast<const char*>(dy) + ((t + 8 * q) * dy_ld + c0) * z, count, BF);
+                    if (act != PSGD_ACT_IDENTITY) b[q] = ld_raw(static_cast<const char*>(pre) + ((t + 8 * q) * pre_ld + c0) * z, count, BF);
+                }
+#pragma unroll
+            for (int q = 0; q < kAhead; ++q) {
+                const int64_t row = t + 8 * q;
+                if (row >= t1) break;
+                float v[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] = widened(a[q], j, BF);   // zero behind the last column
+                if (act != PSGD_ACT_IDENTITY) {
+                    float x[8];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) x[j] = widened(b[q], j, BF);
+                    slope_oct(x, v, act);
+                }
+                if (drop.below) {
+                    const Words r = philox(d, (unsigned)(c0 >> 3), (unsigned)row);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) v[j] = dropped(r, j, drop.below) ? 0.f : v[j];
+                }
+                st_oct<BF>(dz, row * dz_ld + c0, dz_ld - c0 < 8 ? (int)(dz_ld - c0) : 8, v);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) s[j] += v[j];
             }
-            if (drop.below) {
-                const Words r = philox(d, (unsigned)(c0 >> 3), (unsigned)t);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) v[j] = dropped(r, j, drop.below) ? 0.f : v[j];
-            }
-            if (count < 8)   // up to the end of its rows: zero behind the last column
-#pragma unroll
-                for (int j = 0; j < 8; ++j) v[j] = j < count ? v[j] : 0.f;
-            st_oct<BF>(dz, t * dz_ld + c0, dz_ld - c0 < 8 ? (int)(dz_ld - c0) : 8, v);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) s[j] += v[j];
         }
     }
     if (!partial) return;
@@ -111,13 +124,13 @@ bool lay_out(const void* src, int64_t src_ld, bool src_bf, void* dst, int64_t ds
 }
 
 // Whether operands of a bf16 product that cannot go straight to LDS are laid out for it first: a pass over them against slower
-// loads in every tile.  us, laid out / in place: forward, fp32 weights of 8192 x 2048, 300 tokens 38 / 33, 700 49 / 49, 1500 72 / 85, 4000
-// 131 / 194; 4096 x 4095 bf16, both operands, 300 45 / 41, 700 58 / 66, 4000 133 / 201; 2600 x 650 bf16 1500 28 / 19, 4000 46 / 39; 50304 x
-// 2048 fp32 300 218 / 152, 1500 398 / 495.  The weight gradient, which reads the input alone in another place: 1000 x 1001, 4000 tokens
-// 36 / 37, 2600 x 650 1500 26 / 29, 700 17 / 16; 4096 x 4095 300 30 / 33.
+// loads in every tile.  us, laid out / in place: forward, fp32 weights of 8192 x 2048, 300 tokens 34 / 27, 700 44 / 41, 1500 63 / 70, 4000
+// 119 / 165; 50304 x 2048 700 270 / 229, 1500 380 / 444; 4096 x 4095 bf16, both operands, 300 48 / 41, 700 54 / 68, 4000 124 / 196; 2600 x 650
+// bf16 1500 25 / 16, 4000 39 / 32.  The weight gradient, which reads the input alone in another place: 1000 x 1001, 4000 tokens 34 / 31, 2600 x
+// 650 700 14 / 13, 1500 23 / 25, 4000 47 / 64; 4096 x 4095 300 30 / 31, 4000 121 / 192.
 bool lay_out_pays(const LinearCall& c, bool weight_gradient) {
     const double work = (double)c.T * (double)c.n * (double)c.k;
-    return weight_gradient ? work >= 2e9 : c.T >= 640 && work >= 6e9;
+    return weight_gradient ? work >= 2e9 : c.T >= (c.param_bf16 ? 640 : 1000) && work >= 1e10;
 }
 
 // The weights or the input as operand B or A of the product q.M x q.N x q.K
