@@ -147,7 +147,8 @@ PSGD_API psgd_status psgd_plan_offsets(const psgd_plan* plan, int32_t tensor, in
  *                 tiles (128 .. 2048); the whole list for one worker and a set beyond the cache
  *   stream_hints  cache policy of the second and third sweep: -1 (default) by the size of M over all
  *                 workers (non-temporal accesses to M and the error memory above 320 MB; below it, one worker,
- *                 to the momentum and parameters of the fused update where the three together exceed 320 MB),
+ *                 to the momentum and parameters of the fused update where the three together exceed 320 MB; and of the random mask's
+ *                 accesses to the error memory, up to 16 workers),
  *                 0 never, 1 always (M and the error memory).  Resident plans, psgd_step_update: -1 non-temporal accesses to momentum and
  *                 parameters from 4,000,000 elements on (behind other work 2 to 9 % faster than 0; a step repeated on one state with
  *                 nothing in between 3 to 8 % slower), 0 and 1 ordinary ones

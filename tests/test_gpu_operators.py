@@ -559,6 +559,27 @@ def test_random_mask(workers, gdt, odt):
         assert (got[~live.numpy()] == -7.0).all() and (new[:, ~live[:s.n_mat_elems].numpy()] == -7.0).all()
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("workers", [1, 3, 16, 17])
+def test_random_mask_around_the_caches(workers, dtype):
+    """The error memory of large sets goes around the caches: the same bits."""
+    dev = _need_gpu()
+    gen = torch.Generator().manual_seed(workers)
+    res = []
+    for hints in (0, 1):
+        plan = B.Plan(MASK_SHAPES, 2, workers, CODE[dtype], CODE[dtype])
+        plan.set_tuning("stream_hints", hints)
+        s = plan.sizes
+        if not res:
+            grad = torch.randn(workers, s.grad_stride, generator=gen).to(DT[dtype]).to(dev)
+            start = torch.randn(workers, s.err_stride, generator=gen).to(dev)
+        err, out = start.clone(), torch.zeros(s.out_elems, dtype=DT[dtype], device=dev)
+        for step in range(3):
+            plan.random_mask_step(grad, err, 0.4, _rng(dev), out, offset=step, stream=_stream())
+        res.append((err.view(torch.uint8).cpu(), out.view(torch.uint8).cpu()))
+    assert torch.equal(res[0][0], res[1][0]) and torch.equal(res[0][1], res[1][1])
+
+
 def test_random_mask_keeps_the_sum_of_updates():
     """Error feedback loses nothing: after any number of steps, sum of Delta' + mean error = sum of gradients."""
     dev = _need_gpu()
