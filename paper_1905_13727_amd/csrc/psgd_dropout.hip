@@ -11,11 +11,13 @@ namespace psgd {
 // y = residual + D(x).  One lane: eight consecutive columns of a row, one call of the generator.  A workgroup: `high` rows of a band of
 // `wide` groups of eight columns, about kDropItems of them, or one a lane where there are too few for every unit; which row an item lies
 // in is a multiplication (recip = ceil(2^32 / wide), 0 for one group; exact below 2^16 items).
-// Memory bounds it, not the generator: 16384 x 2048 bf16 with a residual 39.5 us, 5.1 TB/s; 8191 x 8191 bf16, rows that begin at any element,
-// 55.6 us, 4.8 TB/s.
+// ONCE: large calls read around the caches, so that those are left to what they write: 16384 x 2048 bf16 with a residual 41 us without, 36.6 with
+// it; 8192 x 2048 20.3 and 19.6, 4096 x 2048 11.2 and 13.8; rows that begin at any element share lines, 8191 x 8191 57 and 60.
+// Memory bounds it, not the generator: 5.5 TB/s and 4.7 for these.
 constexpr int kDropItems = 1024, kDropFew = 256 * kDropItems;
+constexpr int64_t kDropOnceBytes = int64_t(96) << 20;   // read and written
 
-template <bool BF>
+template <bool BF, bool ONCE>
 __global__ __launch_bounds__(kBlock) void k_dropout(const void* x, int64_t x_ld, const void* residual, int64_t residual_ld, void* y,
                                                     int64_t y_ld, int64_t rows, int64_t cols, int wide, int high, unsigned recip,
                                                     int64_t bands, DropArgs drop) {
@@ -28,8 +30,8 @@ __global__ __launch_bounds__(kBlock) void k_dropout(const void* x, int64_t x_ld,
         const int count = (int)(cols - col < 8 ? cols - col : 8);
         if (count <= 0) continue;
         float v[8], z[8];
-        ld_oct<BF>(x, row * x_ld + col, count, v);
-        if (residual) ld_oct<BF>(residual, row * residual_ld + col, count, z);
+        ld_oct<BF, ONCE>(x, row * x_ld + col, count, v);
+        if (residual) ld_oct<BF, ONCE>(residual, row * residual_ld + col, count, z);
         if (drop.below) {
             const Words w = philox(make_draw(words), (unsigned)(col >> 3), (unsigned)row);
 #pragma unroll
@@ -51,7 +53,10 @@ psgd_status launch_dropout(const DropoutCall& c, std::string* what) {
     const unsigned recip = wide > 1 ? (unsigned)(((uint64_t(1) << 32) + wide - 1) / wide) : 0;
     const int64_t bands = (groups + wide - 1) / wide, blocks = (c.rows + high - 1) / high * bands;
     if (blocks > 0x7fffffffLL) return PSGD_EUNSUPPORTED;
-    auto k = c.bf16 ? k_dropout<true> : k_dropout<false>;
+    const int64_t z = c.bf16 ? 2 : 4;
+    auto aligned = [&](const void* p, int64_t ld) { return (reinterpret_cast<uintptr_t>(p) | (uintptr_t)(ld * z)) % 16 == 0; };
+    const bool once = c.rows * c.cols * z * (c.residual ? 3 : 2) >= kDropOnceBytes && aligned(c.x, c.x_ld) && (!c.residual || aligned(c.residual, c.residual_ld));
+    auto k = c.bf16 ? (once ? k_dropout<true, true> : k_dropout<true, false>) : (once ? k_dropout<false, true> : k_dropout<false, false>);
     hipLaunchKernelGGL(k, dim3((unsigned)blocks), dim3(kBlock), 0, static_cast<hipStream_t>(c.stream), c.x, c.x_ld, c.residual,
                        c.residual_ld, c.y, c.y_ld, c.rows, c.cols, wide, high, recip, bands, drop_of(c.drop));
     const hipError_t e = hipGetLastError();

@@ -133,17 +133,28 @@ inline Epilogue epilogue_of(const EpilogueHost& h) {
 typedef unsigned v4u_any __attribute__((ext_vector_type(4), aligned(2)));
 typedef float v4f_any __attribute__((ext_vector_type(4), aligned(4)));
 
+template <bool ONCE>
+__device__ __forceinline__ v4u ld_four(const v4u_any* p) {   // ONCE: around the caches
+    if constexpr (ONCE) return __builtin_nontemporal_load(p);
+    else return *p;
+}
+template <bool ONCE>
+__device__ __forceinline__ v4f ld_four(const v4f_any* p) {
+    if constexpr (ONCE) return __builtin_nontemporal_load(p);
+    else return *p;
+}
+
 // Eight consecutive elements of a row, `count` of which exist
-template <bool BF>
+template <bool BF, bool ONCE = false>
 __device__ __forceinline__ void ld_oct(const void* p, int64_t at, int count, float (&x)[8]) {
     if (count >= 8) {
         if constexpr (BF) {
-            const v4u t = *reinterpret_cast<const v4u_any*>(static_cast<const bf16_t*>(p) + at);
+            const v4u t = ld_four<ONCE>(reinterpret_cast<const v4u_any*>(static_cast<const bf16_t*>(p) + at));
 #pragma unroll
             for (int e = 0; e < 4; ++e) { x[2 * e] = __uint_as_float(t[e] << 16); x[2 * e + 1] = __uint_as_float(t[e] & 0xffff0000u); }
         } else {
-            const v4f lo = *reinterpret_cast<const v4f_any*>(static_cast<const float*>(p) + at);
-            const v4f hi = *reinterpret_cast<const v4f_any*>(static_cast<const float*>(p) + at + 4);
+            const v4f lo = ld_four<ONCE>(reinterpret_cast<const v4f_any*>(static_cast<const float*>(p) + at));
+            const v4f hi = ld_four<ONCE>(reinterpret_cast<const v4f_any*>(static_cast<const float*>(p) + at + 4));
 #pragma unroll
             for (int e = 0; e < 4; ++e) { x[e] = lo[e]; x[4 + e] = hi[e]; }
         }

@@ -507,6 +507,27 @@ def test_dropout_in_place_and_of_infinities(dtype):
     assert set(res.float().unique().tolist()) == {1.0, 7.0}
 
 
+@pytest.mark.parametrize("dtype,rows,cols", [("bf16", 12000, 2048), ("f32", 12289, 1032), ("bf16", 12291, 2052)])
+def test_large_dropout_row_by_row(dtype, rows, cols):
+    """Calls that read around the caches, and one of that size whose rows are not aligned: as the same rows a few at a time."""
+    dev = _need_gpu()
+    gen = torch.Generator(device=dev).manual_seed(rows)
+    x, res = (torch.randn(rows, cols, device=dev, generator=gen).to(DT[dtype]) for _ in range(2))
+    y = torch.empty_like(x)
+    B.dropout_forward(CODE[dtype], rows, cols, x, y, 0.3, _rng(dev), residual=res, stream=_stream())
+    factor = torch.from_numpy(OO.drop_factor(300, cols, 0.3, SEED, OFFSET, first_row=rows - 300)).to(dev)
+    want = OO.dropout(_f64(x[-300:]), factor.cpu().numpy(), _f64(res[-300:]))
+    bound = 2 * V * np.abs(_f64(x[-300:])) * 2 + (U[dtype] + V) * (np.abs(want) + 4 * V * np.abs(_f64(x[-300:]))) + 1e-37
+    near(y[-300:], want, bound)
+    for first in (0, 5000, rows - 64):   # a small call of the first rows draws the same for them
+        if first == 0:
+            z = torch.empty(64, cols, dtype=DT[dtype], device=dev)
+            B.dropout_forward(CODE[dtype], 64, cols, x, z, 0.3, _rng(dev), residual=res, stream=_stream())
+            assert torch.equal(z, y[:64])
+        kept = torch.from_numpy(OO.drop_factor(64, cols, 0.3, SEED, OFFSET, first_row=first) == 0).to(dev)
+        assert torch.equal(y[first:first + 64][kept], res[first:first + 64][kept])
+
+
 def test_dropout_beyond_32_bit_offsets():
     dev = _need_gpu()
     rows, cols = 70000, 33280   # 2.3e9 elements
