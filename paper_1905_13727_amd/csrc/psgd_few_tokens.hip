@@ -5,7 +5,8 @@
 // whatever type and at whatever alignment the parameters have.  Every load takes 64 consecutive bytes of each of sixteen rows, four
 // lanes a row.  Which element of the contraction stands where in an instruction does not matter as long as x, read from the caches,
 // has it in the same place: with fp32 weights and bf16 x a lane's eight are two runs of four.  The waves' sums meet in LDS and are
-// added in the waves' order.
+// added in the waves' order.  What the epilogue needs of memory (bias, residual, the generator's words) is asked for first, so that nothing is
+// waited for behind the sums: one token, 8192 x 2048 bf16 9.0 us with weights from memory, 3.7 TB/s, 10.0 without that.
 #include <hip/hip_runtime.h>
 
 #include "psgd_epilogue.h"

@@ -14,6 +14,12 @@
 // rounded to bf16 on the way.
 // The sums go through LDS once more, 32 rows a wave at a time: a lane then holds eight consecutive columns of a row, one
 // store of sixteen bytes (bf16) and one call of the generator.
+//
+// The matrix instructions bound it: bf16, with bias, 4096 x 8192 x 2048 110 us and 4096 x 8192 x 4096 201 us, 1370 TFLOP/s; 8192 x 50304 x
+// 2048 1365 us, 1240; across 4096 x 8192 x 2048, both gradients together, 217 us, 1270; fp32 4096 x 8192 x 2048 1020 us, 135.  On the
+// largest tile they are busy four fifths of the time (SQ_VALU_MFMA_BUSY_CYCLES over SQ_BUSY_CU_CYCLES); most of the rest is waits at the step's
+// barrier.  Matrix instructions of 32 x 32 x 16 in place of 16 x 16 x 32 lose (4096 x 8192 x 4096 204 -> 223 us), so do four waves of 128 x 128
+// each (their sums and operands do not fit the registers) and workgroups that go on to a next tile (110 -> 113).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -217,7 +223,7 @@ struct Operand {
 constexpr int kLandedAndRead = 0x0070;
 
 // The workgroups that run at the same time on one die (own L2) get neighbouring tiles: numbers are dealt to the eight dies in
-// ranges, and a range goes along the rows of C in bands of eight tiles.
+// ranges, and a range goes along the rows of C in bands of eight tiles (four are as fast, sixteen take 2 to 7 % more).
 __device__ __forceinline__ void tile_of(int number, int count, int tiles_m, int tiles_n, int& tm, int& tn) {
     const int each = count / 8, more = count % 8, die = number % 8;
     int t = die * each + (die < more ? die : more) + number / 8;
@@ -576,13 +582,15 @@ __global__ __launch_bounds__(512, 2) void k_product_two_large(ProductArgs p, Pro
     else product_tile<true, false, false, kStraight, kStraight, 2, 4, 8, 4>(q, block, lds_raw);
 }
 
-// The sum over the splits, in order, and the epilogue.  One lane: eight columns.
+// The sum over the splits, in order, and the epilogue.  One lane: eight columns.  Latency bounds it where it is used, 4 to 6 us a launch, of
+// which 0.5 are memory's for 19 x 2048 outputs of 16 splits; workgroups of one wave put that on as many units as there are.
 template <bool BF>
-__device__ __forceinline__ void join_octs(const ProductArgs& p, int64_t block) {
-    const int64_t per_row = (p.N + 7) / 8, at = block * kWave + threadIdx.x;
+__device__ __forceinline__ void join_octs(const ProductArgs& p, unsigned block) {
+    const unsigned per_row = (unsigned)((p.N + 7) / 8), at = block * kWave + threadIdx.x;   // the sums of all splits are below 2^24
     const DrawWords words = p.ep.drop.below ? words_ahead(p.ep.drop.rng, p.ep.drop.offset) : DrawWords{0, 0, 0, 0};
-    if (at >= p.M * per_row) return;
-    const int64_t i = at / per_row, j = 8 * (at - i * per_row);
+    const unsigned row = at / per_row;
+    if (row >= p.M) return;
+    const int64_t i = row, j = 8 * (int64_t)(at - row * per_row);
     const int count = p.N - j < 8 ? (int)(p.N - j) : 8;
     float v[8] = {}, bias[8];
     const RawOct raw = bias_ahead(p.ep, j, p.N), residual = residual_ahead<BF>(p.ep, i * p.ep.residual_ld + j, count);
@@ -869,7 +877,8 @@ psgd_status launch_backward_products(bool bf16, const ProductCall* x, const Prod
         // if what that costs is less than the launch.
         const Way vx = way_of(*x), vw = way_of(*w);
         const bool sx = vx >= kStraightAcross, sw = vw >= kStraightAcross;
-        // Large ones where that is expected to be faster than each by itself: 4096 x 2048 x 8192 and 8192 x 2048 x 4096 bf16
+        // Large ones where that is expected to be faster than each by itself: 4096 x 2048 x 8192, 128 tiles of twice the length, and 8192 x 2048 x
+        // 4096, 256 tiles, 241 us one after the other and 217 together
         if (sx && sw) {
             const Choice lx = choose(vx, x->M, x->N, x->K, 0), lw = choose(vw, w->M, w->N, w->K, 0);
             const bool x_first = lx.steps_each >= lw.steps_each;
