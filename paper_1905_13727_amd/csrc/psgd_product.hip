@@ -398,8 +398,8 @@ __device__ __forceinline__ void product_tile(const ProductArgs& p, unsigned bloc
         // compiler, as it is where loads go through registers.
         constexpr bool kDeal = BF && AA && BA && AS == kStraight && BS == kStraight;
         const int64_t least = std::min(AA ? K : M, BA ? K : N);
-        const int plain = AS == kStraight || BF == false || least >= 8 ? whole : 0;
-        for (; s + 2 < plain; ++s, buf ^= 1) {
+        const int full = AS == kStraight || !BF || least >= 8 ? whole : 0;
+        for (; s + 2 < full; ++s, buf ^= 1) {
             read(buf, 1, x1, y1);
             multiply(x0, y0);
             if constexpr (kDeal) deal_out<0, MF + NF, MF * NF>();
@@ -464,7 +464,7 @@ __device__ __forceinline__ void product_tile(const ProductArgs& p, unsigned bloc
     // A tile that lies inside C and has neither dropout nor a residual to go through: no choice is left to a row, and a row's place is the
     // lane's fixed offset behind an address that is the same for all.  4096 x 8192 x 2048 bf16 116 us without this, 111 with it.
     constexpr int kOut = BF ? 2 : 4;
-    const bool plain = !partial && !ep.drop.below && !ep.residual && M - i0 >= S::BM && N - j0 >= S::BN && c_ld < (1 << 22) && ep.pre_ld < (1 << 22);
+    const bool plain = !partial && !ep.drop.below && !ep.residual && M - i0 >= S::BM && N - j0 >= S::BN;
     const int64_t row = i0 + wm * MF * 16, col = j0 + wn * NF * 16;
     char* at = static_cast<char*>(c) + (row * c_ld + col) * kOut;
     char* pre = ep.pre ? static_cast<char*>(ep.pre) + (row * ep.pre_ld + col) * kOut : nullptr;

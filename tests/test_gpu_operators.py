@@ -346,6 +346,74 @@ def test_activations_at_infinities():
             assert bool((y[1] == (float("-inf") if act == "identity" else 0.0)).all()), act
 
 
+@pytest.mark.parametrize("act", B.ACTIVATIONS)
+def test_activations_over_their_range(act):
+    """Values and slopes between -14 and 14, every product exact: what the evaluation itself is off by."""
+    dev = _need_gpu()
+    plan = B.Plan([(4, 2)], 1, 1)
+    param = torch.zeros(plan.sizes.out_elems, device=dev)
+    param[0:8:2] = 1.0
+    for T in (29, 40000):
+        x = torch.zeros(T, 2, device=dev)
+        x[:, 0] = torch.linspace(-14, 14, T, device=dev)
+        ws = torch.empty(max(1, plan.linear_workspace(0, T)), dtype=torch.uint8, device=dev)
+        y, pre, dx = torch.empty(T, 4, device=dev), torch.empty(T, 4, device=dev), torch.empty(T, 2, device=dev)
+        plan.linear_forward(0, T, param, x, y, ws, pre=pre, activation=act, stream=_stream())
+        z = _f64(x[:, :1])
+        assert torch.equal(pre, x[:, :1].expand(T, 4))
+        near(y, np.broadcast_to(OO.act(z, act), (T, 4)), (16 * V * (1 + np.abs(z)) + V * np.abs(z)) * np.ones((1, 4)))
+        dy = torch.zeros(T, 4, device=dev)
+        dy[:, 2] = 1.0
+        plan.linear_backward(0, T, param, x, dy, dx, None, ws, pre=pre, activation=act, stream=_stream())
+        near(dx[:, :1], OO.act_slope(z, act), 64 * V * (1 + np.abs(z)) + 2 * V)
+
+
+def near_on_device(got, want, bound):
+    assert bool(torch.isfinite(got).all())
+    worst = float(((got.double() - want).abs() / bound).max())
+    assert worst <= 1.0, "%.3g of the bound" % worst
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("act", B.ACTIVATIONS)
+def test_many_tiles_forward(act, dtype):
+    """Large tiles inside the output and at its edges, a contraction that ends inside a step; against fp64 on the device."""
+    dev = _need_gpu()
+    T, n, k = 4000, 4104, 200
+    L = Layer(n, k, dtype, dtype, dev)
+    x, y, pre = L.normal(T, k), torch.empty(T, n, dtype=DT[dtype], device=dev), torch.empty(T, n, dtype=DT[dtype], device=dev)
+    L.plan.linear_forward(1, T, L.param, x, y, L.workspace(T), pre=pre, activation=act, **L.op())
+    X, W, b = x.double(), L.param[L.w_at:L.w_at + n * k].double().view(n, k), L.param[L.b_at:L.b_at + n].double()
+    z, e = X @ W.T + b, (k + 2) * V * (X.abs() @ W.abs().T + b.abs())
+    near_on_device(pre, z, e + (U[dtype] + 4 * V) * (z.abs() + e) + 1e-37)
+    want = {"identity": lambda v: v, "relu": lambda v: v.clamp(min=0), "gelu": torch.nn.functional.gelu, "silu": torch.nn.functional.silu,
+            "gelu_tanh": lambda v: torch.nn.functional.gelu(v, approximate="tanh")}[act](z)
+    if act != "identity":
+        e = 1.2 * e + 16 * V * (1 + z.abs())
+    near_on_device(y, want, e + (U[dtype] + 4 * V) * (want.abs() + e) + 1e-37)
+
+
+@pytest.mark.parametrize("act,params", [("identity", "bf16"), ("relu", "f32")])
+@pytest.mark.parametrize("T,n,k", [(4096, 3080, 1544), (3000, 2056, 4104), (1500, 4104, 8200)])
+def test_large_gradients(T, n, k, act, params):
+    """Both gradients of large layers, together in one launch and apart; against fp64 on the device."""
+    dev = _need_gpu()
+    L = Layer(n, k, "bf16", params, dev)
+    x, dy, pre = L.normal(T, k), L.normal(T, n), L.normal(T, n)
+    dx, grad = torch.empty(T, k, dtype=torch.bfloat16, device=dev), torch.full((2, L.plan.sizes.grad_stride), -7.0, dtype=torch.bfloat16, device=dev)
+    L.plan.linear_backward(1, T, L.param, x, dy, dx, grad, L.workspace(T), pre=pre if act == "relu" else None, worker=1, activation=act, **L.op())
+    W = L.param[L.w_at:L.w_at + n * k].to(torch.bfloat16).double().view(n, k)
+    dz = dy.double() * (pre > 0) if act == "relu" else dy.double()   # exact in bf16
+    X, u = x.double(), U["bf16"] + 4 * V
+    for got, want, e in ((dx, dz @ W, (n + 2) * V * (dz.abs() @ W.abs())),
+                         (grad[1, L.w_at:L.w_at + n * k].view(n, k), dz.T @ X, (T + 2) * V * (dz.abs().T @ X.abs())),
+                         (grad[1, L.b_at:L.b_at + n], dz.sum(0), (T + 2) * V * dz.abs().sum(0))):
+        near_on_device(got, want, e + u * (want.abs() + e) + 1e-37)
+    grad[1, L.w_at:L.w_at + n * k] = -7.0
+    grad[1, L.b_at:L.b_at + n] = -7.0
+    assert bool((grad == -7.0).all())
+
+
 @pytest.mark.parametrize("T,n,k", [(600, 2304, 520), (2048, 2176, 136)])
 def test_large_layers_in_a_graph(T, n, k):
     """Forward and backward through the largest tiles, captured and replayed three times with eager work between."""
