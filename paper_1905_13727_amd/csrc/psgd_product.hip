@@ -525,6 +525,16 @@ __global__ __launch_bounds__(WM* WN* kWave, 2) void k_product(ProductArgs p) {
     product_tile<BF, AA, BA, AS, BS, WM, WN, MF, NF>(p, blockIdx.x, lds_raw);
 }
 
+// A product p and, in front of it in the same launch, the rows q beyond its last full tile in tiles of 64 rows, divided along the contraction so that
+// each unit has one more short tile.  bf16, in two launches and so: 4099 x 8192 x 2048 122 and 115 us, 4099 x 2048 x 2048 41.5 and 38.8, 4099 x 2048 x
+// 8192 127 and 126.
+template <bool BA, int WM, int WN, int MF, int NF>
+__global__ __launch_bounds__(WM* WN* kWave, 2) void k_product_and_rest(ProductArgs p, ProductArgs q, unsigned first) {
+    extern __shared__ __attribute__((aligned(16))) char lds_raw[];
+    if (blockIdx.x < first) product_tile<true, true, BA, kStraight, kStraight, WM, WN, 2, 2>(q, blockIdx.x, lds_raw);
+    else product_tile<true, true, BA, kStraight, kStraight, WM, WN, MF, NF>(p, blockIdx.x - first, lds_raw);
+}
+
 // The columns' sums over one block of rows and 256 columns; 256 lanes, each eight columns of every eighth row
 template <bool BF>
 __device__ __forceinline__ void sum_block(const ColumnSums& s, unsigned block, char* lds_raw) {
@@ -835,23 +845,50 @@ int64_t product_partial_bytes(bool bf16, int64_t M, int64_t N, int64_t K) {
     return splits > 1 ? std::min(splits * M * N * 4, kMostPartial) : 0;
 }
 
+namespace {
+
+// The rows q beyond the last full tile of p, in one launch with it where p takes the tiles `ch` and q's fill no more than one round.  `done`: so it was.
+psgd_status launch_with_rest(const ProductCall& p, const Choice& ch, const ProductCall& q, bool* done, std::string* what) {
+    typedef Shape<true, true, true, kStraight, kStraight, 2, 4, 8, 4> Large;
+    typedef Shape<true, true, true, kStraight, kStraight, 2, 2, 4, 4> Small;
+    const bool large = ch.kind == 0;
+    const int64_t wide = large ? 128 : 64, steps = (q.K + 63) / 64, tm = (q.M + 63) / 64, tn = (q.N + wide - 1) / wide;
+    const int64_t splits = std::min({kCUs * (int64_t)kTilesAlong[ch.kind].at_once / (tm * tn), steps / kLeastSteps, kMostSplits});
+    *done = splits > 1;
+    if (!*done) return PSGD_OK;
+    const int64_t each = (steps + splits - 1) / splits;
+    const Choice small{2, (steps + each - 1) / each, each, tm, tn, 0};
+    const ProductArgs a = args_of(p, ch), b = args_of(q, small);
+    const unsigned first = (unsigned)(tm * tn * small.splits), all = first + (unsigned)(a.tiles_m * a.tiles_n);
+    auto go = [&](auto k, int lds, int threads) {
+        const hipError_t e = with_lds(k, lds);
+        if (e != hipSuccess) return e;
+        hipLaunchKernelGGL(k, dim3(all), dim3(threads), lds, p.stream, a, b, first);
+        return hipGetLastError();
+    };
+    const hipError_t e = large ? go(p.b_along ? k_product_and_rest<true, 2, 4, 8, 4> : k_product_and_rest<false, 2, 4, 8, 4>, Large::kLds, Large::T)
+                               : go(p.b_along ? k_product_and_rest<true, 2, 2, 4, 4> : k_product_and_rest<false, 2, 2, 4, 4>, Small::kLds, Small::T);
+    const psgd_status st = product_failed(e, what);
+    return st != PSGD_OK ? st : join(true, b, ProductArgs{}, nullptr, p.stream, what);
+}
+
+}  // namespace
+
 psgd_status launch_product(const ProductCall& p, std::string* what) {
     const Way way = way_of(p);
     const Choice ch = choose(way, p.M, p.N, p.K);
     if (ch.tiles_m * ch.tiles_n * ch.splits > 0x7fffffffLL) return PSGD_EUNSUPPORTED;
     // Rows or columns beyond the last full tile cost a row of tiles, which may be the one too many for the last round: a product of
-    // their own, in small tiles, where that is expected to be faster by a tenth.  4099 x 2048 x 8192 bf16 205 us in one, 149 in two.
+    // their own, in small tiles, where that is expected to be faster by a tenth.  4099 x 2048 x 8192 bf16 205 us without.
     if (ch.us > 30) {
         const Rest over = rest_of(way, p.M, p.N, p.K, ch.us, false);
         const int64_t rest = over.count;
         const bool rows = over.rows;
         if (rest) {
             const int64_t z = p.bf16 ? 2 : 4, zb = p.bf16 && !p.b_fp32 ? 2 : 4, zp = p.ep.bias_bf ? 2 : 4;
-            ProductCall q = p;
-            (rows ? q.M : q.N) -= rest;
-            const psgd_status st = launch_product(q, what);
-            if (st != PSGD_OK) return st;
-            const int64_t row = rows ? q.M : 0, col = rows ? 0 : q.N;
+            ProductCall main = p, q = p;
+            (rows ? main.M : main.N) -= rest;
+            const int64_t row = rows ? main.M : 0, col = rows ? 0 : main.N;
             (rows ? q.M : q.N) = rest;
             auto moved = [&](const void* at, int64_t ld, int64_t size) { return at ? static_cast<const char*>(at) + (row * ld + col) * size : nullptr; };
             q.a = static_cast<const char*>(p.a) + (p.a_along ? row * p.a_ld : row) * z;
@@ -862,6 +899,16 @@ psgd_status launch_product(const ProductCall& p, std::string* what) {
             if (p.ep.bias) q.ep.bias = static_cast<const char*>(p.ep.bias) + col * zp;
             q.ep.row0 = p.ep.row0 + row;
             q.ep.col0 = p.ep.col0 + col;
+            if (rows && way >= kStraightAcross && p.a_along) {
+                const Choice cm = choose(way, main.M, main.N, main.K);
+                if (cm.kind < 2 && cm.splits == 1 && (cm.us <= 30 || rest_of(way, main.M, main.N, main.K, cm.us, false).count == 0)) {
+                    bool done;
+                    const psgd_status st = launch_with_rest(main, cm, q, &done, what);
+                    if (st != PSGD_OK || done) return st;
+                }
+            }
+            const psgd_status st = launch_product(main, what);
+            if (st != PSGD_OK) return st;
             return launch_product(q, what);
         }
     }

@@ -393,6 +393,35 @@ def test_many_tiles_forward(act, dtype):
     near_on_device(y, want, e + (U[dtype] + 4 * V) * (want.abs() + e) + 1e-37)
 
 
+@pytest.mark.parametrize("T,n,k", [(4099, 2048, 2048), (4099, 8192, 1032), (4200, 4104, 2048), (4097, 2056, 4096)])
+def test_rows_beyond_the_last_tile(T, n, k):
+    """Ragged batches: forward with dropout and residual, backward of a layer whose input gradient is as ragged; against fp64 on the device."""
+    dev = _need_gpu()
+    L = Layer(n, k, "bf16", "bf16", dev)
+    W, b = L.param[L.w_at:L.w_at + n * k].double().view(n, k), L.param[L.b_at:L.b_at + n].double()
+    x, res, ws, u = L.normal(T, k), L.normal(T, n), L.workspace(T), U["bf16"] + 4 * V
+    y, pre = torch.empty_like(res), torch.empty_like(res)
+    L.plan.linear_forward(1, T, L.param, x, y, ws, pre=pre, activation="relu", **L.op())
+    X = x.double()
+    z, e = X @ W.T + b, (k + 2) * V * (X.abs() @ W.abs().T + b.abs())
+    near_on_device(pre, z, e + u * (z.abs() + e) + 1e-37)
+    e = 1.2 * e + 16 * V * (1 + z.abs())
+    near_on_device(y, z.clamp(min=0), e + u * (z.abs() + e) + 1e-37)
+    L.plan.linear_forward(1, T, L.param, x, y, ws, residual=res, drop=0.25, rng=_rng(dev), **L.op())
+    few = 300
+    for first in (0, T - few):   # the generator's rows are the call's, whichever launch has them
+        rows = slice(first, first + few)
+        factor = torch.from_numpy(OO.drop_factor(few, n, 0.25, SEED, OFFSET, first_row=first)).to(dev)
+        e = (k + 2) * V * (X[rows].abs() @ W.abs().T + b.abs()) * factor
+        want = z[rows] * factor + res[rows].double()
+        near_on_device(y[rows], want, e + u * (want.abs() + e) + 2 * V * res[rows].double().abs() + 2 * V * (z[rows] * factor).abs() + 1e-37)
+    dy, dx = L.normal(T, n), torch.empty(T, k, dtype=torch.bfloat16, device=dev)
+    L.plan.linear_backward(1, T, L.param, None, dy, dx, None, ws, **L.op())
+    dz = dy.double()
+    want, e = dz @ W, (n + 2) * V * (dz.abs() @ W.abs())
+    near_on_device(dx, want, e + u * (want.abs() + e) + 1e-37)
+
+
 @pytest.mark.parametrize("act,params", [("identity", "bf16"), ("relu", "f32")])
 @pytest.mark.parametrize("T,n,k", [(4096, 3080, 1544), (3000, 2056, 4104), (1500, 4104, 8200)])
 def test_large_gradients(T, n, k, act, params):
