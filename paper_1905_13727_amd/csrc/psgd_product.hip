@@ -658,7 +658,7 @@ constexpr int kCUs = 256;
 // The tiles, and what they take: us a step with a unit full, of one tile by itself, and for first loads and epilogue; tiles that a
 // unit holds at once.  Fitted to products of one to four rounds, 128 .. 8192 of the contraction; bf16 both operands straight to LDS along
 // the contraction, and all others (reads across it, loads through registers).  Over 39 bf16 products and every division that was timed the
-// choice takes 0.9 % more than the best one on average, 21 % at most (128 x 2048 x 2048, 14.3 and 11.8 us); over 39 fp32 ones 0.8 and 5 %.
+// choice takes 1.1 % more than the best one on average, 21 % at most (128 x 2048 x 2048, 14.3 and 11.8 us); over 39 fp32 ones 0.8 and 5 %.
 struct TileKind {
     int side;
     int at_once;
