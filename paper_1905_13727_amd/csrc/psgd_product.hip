@@ -222,6 +222,14 @@ struct Operand {
 // s_waitcnt: no load (to LDS too) in flight and every LDS access done
 constexpr int kLandedAndRead = 0x0070;
 
+// Orders a wave's LDS accesses before this point ahead of those behind it, where lanes read what other lanes wrote.  The hardware keeps a wave's
+// LDS accesses in order, so this is no instruction; it keeps the compiler from moving one past another that it can tell apart lane by lane.
+__device__ __forceinline__ void lanes_meet() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 // The workgroups that run at the same time on one die (own L2) get neighbouring tiles: numbers are dealt to the eight dies in
 // ranges, and a range goes along the rows of C in bands of eight tiles (four are as fast, sixteen take 2 to 7 % more).
 __device__ __forceinline__ void tile_of(int number, int count, int tiles_m, int tiles_n, int& tm, int& tn) {
@@ -471,6 +479,7 @@ __device__ __forceinline__ void product_tile(const ProductArgs& p, unsigned bloc
     const unsigned c_lane = (unsigned)(lr * (int)c_ld + 8 * lc) * kOut, pre_lane = (unsigned)(lr * (int)ep.pre_ld + 8 * lc) * kOut;
 #pragma unroll 1
     for (int part = 0; part < MF / 2; ++part) {
+        lanes_meet();   // the part before has been picked up
 #pragma unroll
         for (int q = 0; q < MF / 2; ++q)
             if (q == part)
@@ -481,6 +490,7 @@ __device__ __forceinline__ void product_tile(const ProductArgs& p, unsigned bloc
                         const int r = 16 * m + (lane & 15);
                         *reinterpret_cast<__attribute__((address_space(3))) v4f*>(mine + (r * kQuads + ((4 * n + g) ^ (r & (kQuads - 1)))) * 16) = acc[2 * q + m][n];
                     }
+        lanes_meet();   // this part's sums are there, those of other lanes too
         if (plain) {
             auto finish = [&](auto kind) __attribute__((always_inline)) {
 #pragma unroll
