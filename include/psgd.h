@@ -386,7 +386,8 @@ PSGD_API psgd_status psgd_linear_workspace(const psgd_plan* plan, const psgd_lin
  *                             calls that may run at the same time need workspaces of their own
  * Errors: PSGD_EINVAL for null or misaligned pointers, tensor indices that are not such a matrix or vector, a negative
  * token count, a stride below the row length, drop outside [0, 1]; PSGD_EUNSUPPORTED for more than 2^20 rows or
- * columns or a larger stride, more than 2^30 tokens, bf16 parameters on a plan with fp32 gradients. */
+ * columns or a larger stride, more than 2^30 tokens, more than 2^37 elements of x, y or the weights, bf16 parameters on a
+ * plan with fp32 gradients. */
 PSGD_API psgd_status psgd_linear_forward(psgd_plan* plan, const psgd_linear* op, const void* param, const void* x,
                                          const void* residual, void* pre, void* y, void* workspace, void* hip_stream);
 
@@ -401,15 +402,16 @@ PSGD_API psgd_status psgd_linear_forward(psgd_plan* plan, const psgd_linear* op,
  *                             (x may then be NULL)
  *   accumulate                1: dW and db are added to what grad holds (micro-batches, a weight used twice)
  * tokens = 0: dW and db are set to zero unless accumulate.  Same errors; PSGD_EINVAL also for a worker outside
- * [0, W) and for dx and grad both NULL. */
+ * [0, W) and for dx and grad both NULL, PSGD_EUNSUPPORTED also for more than 2^30 - 64 tokens (unless with the identity, without
+ * dropout and without a bias gradient).  A refused call has launched nothing. */
 PSGD_API psgd_status psgd_linear_backward(psgd_plan* plan, const psgd_linear* op, const void* param, const void* x,
                                           const void* pre, const void* dy, void* dx, void* grad, int32_t worker,
                                           int32_t accumulate, void* workspace, void* hip_stream);
 
 /* y = residual + D(x) over [rows][cols] of `dtype`, and dx = D(dy).  residual may be NULL; y may be x or residual, dx may
  * be dy (the same stride).  rows or cols may be 0.  Errors: PSGD_EINVAL for null or misaligned pointers, negative sizes,
- * strides below cols, p outside [0, 1]; PSGD_EUNSUPPORTED for sizes or strides of 2^31 and more, or more than 2^42
- * elements. */
+ * strides below cols, p outside [0, 1]; PSGD_EUNSUPPORTED for sizes or strides of 2^31 and more, or more elements than one
+ * launch takes: never up to 2^36, always above 2^37. */
 PSGD_API psgd_status psgd_dropout_forward(psgd_dtype dtype, int64_t rows, int64_t cols, const void* x, int64_t x_stride,
                                           const void* residual, int64_t residual_stride, void* y, int64_t y_stride,
                                           double p, const uint64_t* rng, uint64_t offset, void* hip_stream);
@@ -429,7 +431,8 @@ PSGD_API psgd_status psgd_dropout_backward(psgd_dtype dtype, int64_t rows, int64
  *   grad    (device, const)  as psgd_step, err (device, in/out) in: e_w ; out: e_w <- M_w - Delta'
  *   out     (device, out)    [N+L] out_dtype: Delta'
  * grad, err and out are aligned to four elements.  Errors: PSGD_EINVAL for null or misaligned pointers, keep above 1 or
- * NaN; PSGD_EUNSUPPORTED for a matrix of more than 2^34 entries. */
+ * NaN; PSGD_EUNSUPPORTED for plans of 2^34 elements or more (the matrices counted in slices of 1024), and with the plan's budget where
+ * that is 2^32 entries of a matrix or more. */
 PSGD_API psgd_status psgd_random_mask_step(psgd_plan* plan, const void* grad, float* err, double keep, const uint64_t* rng,
                                            uint64_t offset, void* out, void* hip_stream);
 

@@ -52,7 +52,7 @@ psgd_status launch_dropout(const DropoutCall& c, std::string* what) {
     const int high = wide < items ? items / wide : 1;
     const unsigned recip = wide > 1 ? (unsigned)(((uint64_t(1) << 32) + wide - 1) / wide) : 0;
     const int64_t bands = (groups + wide - 1) / wide, blocks = (c.rows + high - 1) / high * bands;
-    if (blocks > 0x7fffffffLL) return PSGD_EUNSUPPORTED;
+    if (blocks > most_groups(kBlock)) return PSGD_EUNSUPPORTED;   // more than 2^36 elements
     const int64_t z = c.bf16 ? 2 : 4;
     auto aligned = [&](const void* p, int64_t ld) { return (reinterpret_cast<uintptr_t>(p) | (uintptr_t)(ld * z)) % 16 == 0; };
     const bool once = c.rows * c.cols * z * (c.residual ? 3 : 2) >= kDropOnceBytes && aligned(c.x, c.x_ld) && (!c.residual || aligned(c.residual, c.residual_ld));
@@ -189,18 +189,18 @@ __global__ __launch_bounds__(kBlock) void k_random_mask(const MatDesc* __restric
 psgd_status launch_random_mask(psgd_plan* plan, const void* grad, float* err, double keep, const uint64_t* rng, uint64_t offset,
                                void* out, void* stream) {
     for (const MatDesc& d : plan->mats)
-        if ((int64_t)d.n * d.m > (int64_t(1) << 34) || d.kept >= (int64_t(1) << 32)) {
-            plan->last_error = "random mask: a matrix of more than 2^34 entries";
+        if (keep < 0 && d.kept >= (int64_t(1) << 32)) {
+            plan->last_error = "random mask: a budget of 2^32 entries of a matrix or more";
             return PSGD_EUNSUPPORTED;
         }
+    const int64_t slices = plan->flat_tiles + plan->flat_vec_tiles;   // fewer than 2^24, so a matrix has fewer than 2^34 entries too
+    if (slices > most_groups(kBlock)) {
+        plan->last_error = "random mask: 2^34 elements or more";
+        return PSGD_EUNSUPPORTED;
+    }
     if (!plan->uploaded) {
         psgd_status st = upload_tables(plan);
         if (st != PSGD_OK) return st;
-    }
-    const int64_t slices = plan->flat_tiles + plan->flat_vec_tiles;
-    if (slices > 0x7fffffffLL) {
-        plan->last_error = "random mask: more than 2^31 slices of 1024 elements";
-        return PSGD_EUNSUPPORTED;
     }
     if (slices == 0) return PSGD_OK;
     const uint64_t threshold = keep < 0 ? 0 : (uint64_t)(keep * 4294967296.0 + 0.5);

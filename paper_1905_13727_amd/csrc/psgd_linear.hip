@@ -130,7 +130,8 @@ bool lay_out(const void* src, int64_t src_ld, bool src_bf, void* dst, int64_t ds
 // 119 / 165; 50304 x 2048 700 270 / 229, 1500 380 / 444; 4096 x 4095 bf16, both operands, 300 48 / 41, 700 54 / 68, 4000 124 / 196; 2600 x 650
 // bf16 1500 25 / 16, 4000 39 / 32.  The weight gradient, which reads the input alone in another place: 1000 x 1001, 4000 tokens 34 / 31, 2600 x
 // 650 700 14 / 13, 1500 23 / 25, 4000 47 / 64; 4096 x 4095 300 30 / 31, 4000 121 / 192.
-bool lay_out_pays(const LinearCall& c, bool weight_gradient) {
+bool lay_out_pays(const LinearCall& c, int64_t rows, int64_t ld, bool weight_gradient) {
+    if ((rows * (ld / 8) + kBlock - 1) / kBlock > most_groups(kBlock)) return false;   // more than one launch takes: 64 GiB
     const double work = (double)c.T * (double)c.n * (double)c.k;
     return weight_gradient ? work >= 2e9 : c.T >= (c.param_bf16 ? 640 : 1000) && work >= 1e10;
 }
@@ -141,7 +142,7 @@ bool weights(const LinearCall& c, const Parts& p, ProductCall& q, std::string* w
     q.b_ld = c.k;
     q.b_fp32 = c.bf16 && !c.param_bf16;
     q.b_ready = !q.b_fp32 && c.k % 8 == 0;
-    if (!c.bf16 || q.b_ready || !lay_out_pays(c, false)) return true;
+    if (!c.bf16 || q.b_ready || !lay_out_pays(c, c.n, p.k_ld, false)) return true;
     void* to = static_cast<char*>(c.workspace) + p.w;
     q.b = to;
     q.b_ld = p.k_ld;
@@ -153,7 +154,7 @@ bool input(const LinearCall& c, const Parts& p, const ProductCall& q, const void
     *x = c.x;
     *ld = c.x_ld;
     *ready = vec_aligned(c.x, c.x_ld) && c.k % 8 == 0;
-    if (!c.bf16 || *ready || !lay_out_pays(c, !q.a_along)) return true;
+    if (!c.bf16 || *ready || !lay_out_pays(c, c.T, p.k_ld, !q.a_along)) return true;
     void* to = static_cast<char*>(c.workspace) + p.x;
     *x = to;
     *ld = p.k_ld;
@@ -201,13 +202,14 @@ psgd_status launch_linear_backward(const LinearCall& c, std::string* what) {
     const Parts p = parts_of(c);
     const float scale = c.drop.below ? c.drop.factor : 1.f;
     if (c.T == 0 && c.accumulate) return PSGD_OK;
+    const bool direct = c.act == PSGD_ACT_IDENTITY && !c.drop.below;   // dz is dy
     char* const ws = static_cast<char*>(c.workspace);
     const int64_t blocks = up(c.T, kSumRows) / kSumRows;
+    if ((!direct || c.db) && (c.n + 255) / 256 * blocks > most_groups(kBlock)) return PSGD_EUNSUPPORTED;   // before anything is launched
     const void* dz = c.dy;
     int64_t dz_ld = c.dy_ld;
     bool dz_ready = false;
     if (c.T > 0) {
-        const bool direct = c.act == PSGD_ACT_IDENTITY && !c.drop.below;
         if (!direct) {   // rows padded with zeros to multiples of sixteen bytes
             dz = ws + p.dz;
             dz_ld = p.n_ld;
@@ -215,7 +217,6 @@ psgd_status launch_linear_backward(const LinearCall& c, std::string* what) {
         dz_ready = !direct || (vec_aligned(c.dy, c.dy_ld) && c.n % 8 == 0);
         if (!direct) {
             auto k = c.bf16 ? k_dz<true> : k_dz<false>;
-            if ((c.n + 255) / 256 * blocks > 0x7fffffffLL) return PSGD_EUNSUPPORTED;
             hipLaunchKernelGGL(k, dim3((unsigned)((c.n + 255) / 256 * blocks)), dim3(kBlock), 0, s, c.dy, c.dy_ld, c.pre, c.pre_ld, c.act, drop_of(c.drop),
                                const_cast<void*>(dz), dz_ld, c.db ? reinterpret_cast<float*>(ws + p.db) : nullptr, c.T, c.n);
             if (failed("k_dz", what)) return PSGD_EHIP;

@@ -1,4 +1,5 @@
 // C entry points of the operators around the compressor step: checks of the arguments, nothing else.  Host only.
+#include <algorithm>
 #include <cmath>
 #include <new>
 
@@ -51,6 +52,8 @@ psgd_status linear_args(const psgd_plan* plan, const psgd_linear* op, LinearCall
     for (int64_t v : {c->n, c->k, c->x_ld, c->dx_ld, c->residual_ld, c->pre_ld, c->y_ld, c->dy_ld})
         if (v > psgd::kLinMaxDim) return PSGD_EUNSUPPORTED;
     if (c->T > psgd::kLinMaxTokens) return PSGD_EUNSUPPORTED;
+    const int64_t widest = std::max(c->n, c->k);
+    if (c->T > psgd::kLinMaxElems / widest || c->n > psgd::kLinMaxElems / c->k) return PSGD_EUNSUPPORTED;
     return PSGD_OK;
 }
 
@@ -150,7 +153,7 @@ static psgd_status dropout(psgd_dtype dtype, int64_t rows, int64_t cols, const v
         return PSGD_EINVAL;
     for (int64_t v : {rows, cols, c.x_ld, c.residual_ld, c.y_ld})
         if (v > 0x7fffffffLL) return PSGD_EUNSUPPORTED;
-    if (rows > 0 && cols > (int64_t(1) << 42) / rows) return PSGD_EUNSUPPORTED;
+    if (rows > 0 && cols > (int64_t(1) << 37) / rows) return PSGD_EUNSUPPORTED;   // more than any launch takes
     if (rows == 0 || cols == 0) return PSGD_OK;
     c.bf16 = dtype == PSGD_BF16;
     const size_t z = c.bf16 ? 2 : 4;

@@ -11,6 +11,10 @@ namespace psgd {
 
 constexpr int64_t kLinMaxDim = int64_t(1) << 20;      // rows, columns and strides: a tile of 256 rows of fp32 stays below 2^31 bytes
 constexpr int64_t kLinMaxTokens = int64_t(1) << 30;
+constexpr int64_t kLinMaxElems = int64_t(1) << 37;    // of x, y and the weights: then the products' tiles fit a launch (choose)
+
+// The most workgroups of a launch: its lanes are counted in 32 bits
+constexpr int64_t most_groups(int lanes) { return 0xffffffffLL / lanes; }
 
 struct DropHost {
     const uint64_t* rng;

@@ -674,6 +674,7 @@ struct TileKind {
     int at_once;
     double full, alone, ends;
 };
+constexpr int lanes_of(int kind) { return kind == 0 ? 512 : 256; }
 constexpr TileKind kTilesAlong[] = {{256, 1, 1.2, 1.2, 9}, {128, 2, 0.41, 0.42, 5.7}, {64, 4, 0.138, 0.204, 3.5}};
 constexpr TileKind kTilesAcross[] = {{256, 1, 1.36, 1.36, 8.5}, {128, 2, 0.465, 0.735, 4.4}, {64, 4, 0.163, 0.46, 2.9}};
 constexpr TileKind kTilesFp32[] = {{256, 1, 0, 0, 0}, {128, 2, 1.9, 2.4, 5}, {64, 4, 0.5, 0.8, 3}};   // none of 256
@@ -692,15 +693,18 @@ struct Choice {
 };
 
 // The tile and the division of the contraction with the least expected time: steps of a tile one after the other, as many tiles
-// at a time as the units hold, and the sums of the splits written and read again.
+// at a time as the units hold, and the sums of the splits written and read again.  One launch takes the tiles: those of 64 where they are few
+// enough, and those of 128 of any product of up to kLinMaxElems outputs.
 Choice choose(Way way, int64_t M, int64_t N, int64_t K, int only = -1) {
     const int64_t step = way == kInFp32 ? 32 : 64, steps = (K + step - 1) / step;
+    const bool small_fit = ((M + 63) / 64) * ((N + 63) / 64) <= most_groups(lanes_of(2));
     Choice best{-1, 0, 0, 0, 0, 0};
     for (int kind = 0; kind < 3; ++kind) {
         const TileKind& t = tile_kind(way, kind);
         if ((kind == 0 && way < kStraightAcross) || (only >= 0 && kind != only)) continue;
-        if (only < 0 && t.side > 64 && (M <= t.side / 2 || N <= t.side / 2)) continue;   // more than half of every tile outside
+        if (only < 0 && t.side > 64 && (M <= t.side / 2 || N <= t.side / 2) && small_fit) continue;   // more than half of every tile outside
         const int64_t tm = (M + t.side - 1) / t.side, tn = (N + t.side - 1) / t.side, tiles = tm * tn;
+        if (only < 0 && kind == 2 && !small_fit) continue;
         for (int64_t splits = 1; splits <= (kind == 0 ? 1 : kMostSplits) && (splits == 1 || (splits <= steps / kLeastSteps && tiles * splits <= kCUs * t.at_once)); ++splits) {
             const int64_t each = std::max<int64_t>(1, (steps + splits - 1) / splits), parts = std::max<int64_t>(1, (steps + each - 1) / each);
             if (parts != splits) continue;
@@ -833,7 +837,6 @@ psgd_status join(bool bf16, const ProductArgs& p, const ProductArgs& q, const Co
 psgd_status sum_blocks_alone(bool bf16, const ColumnSums* sums, hipStream_t stream, std::string* what) {
     const int64_t blocks = sum_blocks(sums);
     if (!blocks) return PSGD_OK;
-    if (blocks > 0x7fffffffLL) return PSGD_EUNSUPPORTED;
     auto k = bf16 ? k_sum_blocks<true> : k_sum_blocks<false>;
     hipLaunchKernelGGL(k, dim3((unsigned)blocks), dim3(256), 0, stream, *sums);
     const hipError_t e = hipGetLastError();
@@ -864,7 +867,7 @@ psgd_status launch_with_rest(const ProductCall& p, const Choice& ch, const Produ
     const bool large = ch.kind == 0;
     const int64_t wide = large ? 128 : 64, steps = (q.K + 63) / 64, tm = (q.M + 63) / 64, tn = (q.N + wide - 1) / wide;
     const int64_t splits = std::min({kCUs * (int64_t)kTilesAlong[ch.kind].at_once / (tm * tn), steps / kLeastSteps, kMostSplits});
-    *done = splits > 1;
+    *done = splits > 1 && ch.tiles_m * ch.tiles_n + tm * tn * splits <= most_groups(lanes_of(ch.kind));
     if (!*done) return PSGD_OK;
     const int64_t each = (steps + splits - 1) / splits;
     const Choice small{2, (steps + each - 1) / each, each, tm, tn, 0};
@@ -887,7 +890,6 @@ psgd_status launch_with_rest(const ProductCall& p, const Choice& ch, const Produ
 psgd_status launch_product(const ProductCall& p, std::string* what) {
     const Way way = way_of(p);
     const Choice ch = choose(way, p.M, p.N, p.K);
-    if (ch.tiles_m * ch.tiles_n * ch.splits > 0x7fffffffLL) return PSGD_EUNSUPPORTED;
     // Rows or columns beyond the last full tile cost a row of tiles, which may be the one too many for the last round: a product of
     // their own, in small tiles, where that is expected to be faster by a tenth.  4099 x 2048 x 8192 bf16 205 us without.
     if (ch.us > 30) {
@@ -941,7 +943,7 @@ psgd_status launch_backward_products(bool bf16, const ProductCall* x, const Prod
             const bool x_first = lx.steps_each >= lw.steps_each;
             const int64_t first = (x_first ? lx : lw).tiles_m * (x_first ? lx : lw).tiles_n, all = lx.tiles_m * lx.tiles_n + lw.tiles_m * lw.tiles_n;
             const double apart = product_us(vx, x->M, x->N, x->K) + product_us(vw, w->M, w->N, w->K);
-            if (apart > 60 && all <= 0x7fffffffLL && two_large_us(x_first ? lx : lw, x_first ? lw : lx) < 0.95 * apart) {
+            if (apart > 60 && all <= most_groups(lanes_of(0)) && two_large_us(x_first ? lx : lw, x_first ? lw : lx) < 0.95 * apart) {
                 if (const psgd_status st = sum_blocks_alone(bf16, sums, stream, what); st != PSGD_OK) return st;
                 typedef Shape<true, true, false, kStraight, kStraight, 2, 4, 8, 4> S;
                 hipError_t e = with_lds(k_product_two_large, S::kLds);
@@ -962,7 +964,7 @@ psgd_status launch_backward_products(bool bf16, const ProductCall* x, const Prod
             }
         }
         const int64_t blocks = cx.tiles_m * cx.tiles_n * cx.splits + cw.tiles_m * cw.tiles_n * cw.splits + sum_blocks(sums);
-        if (cx.kind == cw.kind && cx.kind > 0 && cx.us + cw.us < 150 && blocks < 0x7fffffffLL) {
+        if (cx.kind == cw.kind && cx.kind > 0 && cx.us + cw.us < 150 && blocks <= most_groups(lanes_of(cx.kind))) {
             const ProductArgs p = args_of(*x, cx), q = args_of(*w, cw);
             const hipError_t e = !bf16 ? start_two<false, kFp32, kFp32, kFp32>(p, q, sums, cx.kind, stream)
                                  : sx && sw ? start_two<true, kStraight, kStraight, kStraight>(p, q, sums, cx.kind, stream)
