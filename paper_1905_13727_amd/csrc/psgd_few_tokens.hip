@@ -180,26 +180,6 @@ __global__ __launch_bounds__(kFewWaves* kWave, TF == 1 ? 4 : 2) void k_few_token
     }
 }
 
-// Where this takes less time than the tiles of the other products, which read x once for 64 rows of W and divide the contraction
-// over the chip: us, this / tiles, one, 16 and 32 tokens, n x k.
-//   fp32: 650 x 650 4.3 / 9.7, 4.6 / 9.8, 6.4 / 10.1; 8192 x 2048 12.9 / 24.9, 16.9 / 25.3, 18.4 / 26.2; 50304 x 2048 82 / 137, 107 / 137, 119 / 138;
-//   2048 x 8192, short of workgroups, 20.5 / 25.9, 30.4 / 26.3, 44.5 / 26.8; 512 x 8192 19.6 / 13.3.
-//   bf16: 512 x 512 2.9 / 4.6, 3.3 / 4.7, 3.7 / 5.0; 2048 x 2048 4.4 / 6.6, 5.8 / 7.0, 7.5 / 7.6; 8192 x 2048 6.6 / 9.9, 7.9 / 16.1, 9.8 / 16.6; beyond
-//   2^24 weights it loses: 8192 x 4096 16.3 / 15.0, 16.4 / 15.7, 17.9 / 16.5; 50304 x 2048 39 / 31, 44 / 32, 52 / 34; and where n is small or
-//   rows of odd length begin between words: 2048 x 8192 11.6 / 10.6, 16.6 / 12.1, 23.6 / 13.0; 1000 x 1001 6.5 / 7.2, 8.7 / 7.9, 11.5 / 8.1; 4096 x
-//   4095 18.7 / 11.5, 30.3 / 13.0, 43.4 / 13.7.
-//   bf16, fp32 weights: 512 x 512 3.4 / 6.0, 4.1 / 6.0, 5.0 / 6.5; 1000 x 1001 4.8 / 7.4, 6.6 / 8.0, 9.4 / 8.2; 2048 x 2048 6.9 / 7.5, 9.5 / 8.0, 13.0 / 8.6;
-//   8192 x 2048 12.5 / 15.1, 16.8 / 15.9, 18.9 / 16.6; 50304 x 2048 69 / 103, 97 / 105, 109 / 108.
-bool few_tokens(const LinearCall& c) {
-    if (c.T > kFewTokens) return false;
-    const int64_t weights = c.n * c.k;
-    const bool one = c.T <= 4, some = c.T <= 16;
-    if (!c.bf16) return 2 * c.n >= c.k || (one && 4 * c.n >= c.k);
-    if (2 * c.n < c.k) return false;
-    if (!c.param_bf16) return one || weights <= (some ? 1 << 20 : 1 << 19);
-    return c.k % 2 ? one && weights <= 1 << 21 : weights <= 1 << 24;
-}
-
 namespace {
 
 template <bool BF, bool WBF>

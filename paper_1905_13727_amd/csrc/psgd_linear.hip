@@ -86,16 +86,12 @@ __global__ __launch_bounds__(kBlock) void k_dz(const void* dy, int64_t dy_ld, co
 
 namespace {
 
-int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b * b; }
-
 bool failed(const char* name, std::string* what) {
     const hipError_t e = hipGetLastError();
     if (e == hipSuccess) return false;
     *what = std::string("launch ") + name + ": " + hipGetErrorString(e);
     return true;
 }
-
-bool vec_aligned(const void* p, int64_t ld) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld % 8 == 0; }   // bf16
 
 // Where the parts of the workspace are
 struct Parts {
@@ -125,40 +121,28 @@ bool lay_out(const void* src, int64_t src_ld, bool src_bf, void* dst, int64_t ds
     return !failed("k_lay_out", what);
 }
 
-// Whether operands of a bf16 product that cannot go straight to LDS are laid out for it first: a pass over them against slower
-// loads in every tile.  us, laid out / in place: forward, fp32 weights of 8192 x 2048, 300 tokens 34 / 27, 700 44 / 41, 1500 63 / 70, 4000
-// 119 / 165; 50304 x 2048 700 270 / 229, 1500 380 / 444; 4096 x 4095 bf16, both operands, 300 48 / 41, 700 54 / 68, 4000 124 / 196; 2600 x 650
-// bf16 1500 25 / 16, 4000 39 / 32.  The weight gradient, which reads the input alone in another place: 1000 x 1001, 4000 tokens 34 / 31, 2600 x
-// 650 700 14 / 13, 1500 23 / 25, 4000 47 / 64; 4096 x 4095 300 30 / 31, 4000 121 / 192.
-bool lay_out_pays(const LinearCall& c, int64_t rows, int64_t ld, bool weight_gradient) {
-    if ((rows * (ld / 8) + kBlock - 1) / kBlock > most_groups(kBlock)) return false;   // more than one launch takes: 64 GiB
-    const double work = (double)c.T * (double)c.n * (double)c.k;
-    return weight_gradient ? work >= 2e9 : c.T >= (c.param_bf16 ? 640 : 1000) && work >= 1e10;
-}
-
 // The weights or the input as operand B or A of the product q.M x q.N x q.K
 bool weights(const LinearCall& c, const Parts& p, ProductCall& q, std::string* what) {
+    const Comes w = weights_come(c);
     q.b = c.w;
     q.b_ld = c.k;
-    q.b_fp32 = c.bf16 && !c.param_bf16;
-    q.b_ready = !q.b_fp32 && c.k % 8 == 0;
-    if (!c.bf16 || q.b_ready || !lay_out_pays(c, c.n, p.k_ld, false)) return true;
+    q.b_fp32 = c.bf16 && !c.param_bf16 && !w.lay;
+    q.b_ready = w.ready || w.lay;
+    if (!w.lay) return true;
     void* to = static_cast<char*>(c.workspace) + p.w;
     q.b = to;
     q.b_ld = p.k_ld;
-    q.b_fp32 = false;
-    q.b_ready = true;
     return lay_out(c.w, c.k, c.param_bf16, to, p.k_ld, c.n, c.k, q.stream, what);
 }
 bool input(const LinearCall& c, const Parts& p, const ProductCall& q, const void** x, int64_t* ld, bool* ready, std::string* what) {
+    const Comes in = input_comes(c, !q.a_along);
     *x = c.x;
     *ld = c.x_ld;
-    *ready = vec_aligned(c.x, c.x_ld) && c.k % 8 == 0;
-    if (!c.bf16 || *ready || !lay_out_pays(c, c.T, p.k_ld, !q.a_along)) return true;
+    *ready = in.ready || in.lay;
+    if (!in.lay) return true;
     void* to = static_cast<char*>(c.workspace) + p.x;
     *x = to;
     *ld = p.k_ld;
-    *ready = true;
     return lay_out(c.x, c.x_ld, true, to, p.k_ld, c.T, c.k, q.stream, what);
 }
 
@@ -214,7 +198,7 @@ psgd_status launch_linear_backward(const LinearCall& c, std::string* what) {
             dz = ws + p.dz;
             dz_ld = p.n_ld;
         }
-        dz_ready = !direct || (vec_aligned(c.dy, c.dy_ld) && c.n % 8 == 0);
+        dz_ready = dz_comes(c, direct).ready;
         if (!direct) {
             auto k = c.bf16 ? k_dz<true> : k_dz<false>;
             hipLaunchKernelGGL(k, dim3((unsigned)((c.n + 255) / 256 * blocks)), dim3(kBlock), 0, s, c.dy, c.dy_ld, c.pre, c.pre_ld, c.act, drop_of(c.drop),

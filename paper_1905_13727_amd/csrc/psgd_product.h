@@ -6,7 +6,7 @@
 
 #include <string>
 
-#include "psgd_operators.h"
+#include "psgd_linear_rules.h"
 
 namespace psgd {
 
@@ -50,7 +50,6 @@ psgd_status launch_product(const ProductCall& c, std::string* what);
 
 // The bias gradient: sums of the columns over blocks of kSumRows rows, [ceil(T / kSumRows)][n], added up and written (or added) to db.
 // With `dy` the blocks' sums are of that array and still to be computed, otherwise `sums` holds them.
-constexpr int kSumRows = 64;
 struct ColumnSums {
     const void* dy;
     int64_t dy_ld, T, n;
@@ -64,9 +63,7 @@ struct ColumnSums {
 psgd_status launch_backward_products(bool bf16, const ProductCall* x, const ProductCall* w, const ColumnSums* sums, hipStream_t stream,
                                      std::string* what);
 
-// The forward product of at most kFewTokens tokens, without scratch and whatever the operands' types and alignment
-constexpr int64_t kFewTokens = 32;
-bool few_tokens(const LinearCall& c);
+// The forward product where few_tokens says so
 psgd_status launch_few_tokens(const LinearCall& c, const EpilogueHost& ep, std::string* what);
 
 }  // namespace psgd

@@ -663,107 +663,6 @@ __global__ __launch_bounds__(kWave) void k_join(ProductArgs p, int64_t p_blocks,
 
 namespace {
 
-constexpr int kCUs = 256;
-
-// The tiles, and what they take: us a step with a unit full, of one tile by itself, and for first loads and epilogue; tiles that a
-// unit holds at once.  Fitted to products of one to four rounds, 128 .. 8192 of the contraction; bf16 both operands straight to LDS along
-// the contraction, and all others (reads across it, loads through registers).  Over 39 bf16 products and every division that was timed the
-// choice takes 1.1 % more than the best one on average, 21 % at most (128 x 2048 x 2048, 14.3 and 11.8 us); over 39 fp32 ones 0.8 and 5 %.
-struct TileKind {
-    int side;
-    int at_once;
-    double full, alone, ends;
-};
-constexpr int lanes_of(int kind) { return kind == 0 ? 512 : 256; }
-constexpr TileKind kTilesAlong[] = {{256, 1, 1.2, 1.2, 9}, {128, 2, 0.41, 0.42, 5.7}, {64, 4, 0.138, 0.204, 3.5}};
-constexpr TileKind kTilesAcross[] = {{256, 1, 1.36, 1.36, 8.5}, {128, 2, 0.465, 0.735, 4.4}, {64, 4, 0.163, 0.46, 2.9}};
-constexpr TileKind kTilesFp32[] = {{256, 1, 0, 0, 0}, {128, 2, 1.9, 2.4, 5}, {64, 4, 0.5, 0.8, 3}};   // none of 256
-// How a product's operands come
-enum Way { kInFp32, kByRegisters, kStraightAcross, kStraightAlong };
-const TileKind& tile_kind(Way way, int kind) { return (way == kInFp32 ? kTilesFp32 : way == kStraightAlong ? kTilesAlong : kTilesAcross)[kind]; }
-
-// A split takes four steps at least, and there are no more tiles and splits than the units hold at a time, so that the sums
-// take at most 64 MiB whatever the sizes.
-constexpr int64_t kMostSplits = 32, kLeastSteps = 4, kMostPartial = int64_t(kCUs) * 256 * 256 * 4;
-
-struct Choice {
-    int kind;          // of the tiles
-    int64_t splits, steps_each, tiles_m, tiles_n;
-    double us;         // expected
-};
-
-// The tile and the division of the contraction with the least expected time: steps of a tile one after the other, as many tiles
-// at a time as the units hold, and the sums of the splits written and read again.  One launch takes the tiles: those of 64 where they are few
-// enough, and those of 128 of any product of up to kLinMaxElems outputs.
-Choice choose(Way way, int64_t M, int64_t N, int64_t K, int only = -1) {
-    const int64_t step = way == kInFp32 ? 32 : 64, steps = (K + step - 1) / step;
-    const bool small_fit = ((M + 63) / 64) * ((N + 63) / 64) <= most_groups(lanes_of(2));
-    Choice best{-1, 0, 0, 0, 0, 0};
-    for (int kind = 0; kind < 3; ++kind) {
-        const TileKind& t = tile_kind(way, kind);
-        if ((kind == 0 && way < kStraightAcross) || (only >= 0 && kind != only)) continue;
-        if (only < 0 && t.side > 64 && (M <= t.side / 2 || N <= t.side / 2) && small_fit) continue;   // more than half of every tile outside
-        const int64_t tm = (M + t.side - 1) / t.side, tn = (N + t.side - 1) / t.side, tiles = tm * tn;
-        if (only < 0 && kind == 2 && !small_fit) continue;
-        for (int64_t splits = 1; splits <= (kind == 0 ? 1 : kMostSplits) && (splits == 1 || (splits <= steps / kLeastSteps && tiles * splits <= kCUs * t.at_once)); ++splits) {
-            const int64_t each = std::max<int64_t>(1, (steps + splits - 1) / splits), parts = std::max<int64_t>(1, (steps + each - 1) / each);
-            if (parts != splits) continue;
-            // tiles a unit works off: full loads, and what is left, which does not spread evenly
-            const int64_t n = tiles * splits, batches = n / (kCUs * t.at_once), rest = n % (kCUs * t.at_once);
-            const double left = rest == 0 ? 0 : std::max<double>((double)((rest + kCUs - 1) / kCUs), batches ? 0.8 * t.at_once : 0);
-            const double work = batches * t.at_once + left;
-            double us = each * std::max(t.alone, work * t.full) + t.ends * std::max<double>(1, work / std::min(t.at_once, 2));
-            if (splits > 1) us += 4.2 + 1.6e-6 * splits * M * N;
-            if (best.kind < 0 || us < best.us) best = Choice{kind, splits, each, tm, tn, us};
-        }
-    }
-    return best;
-}
-
-// Rows (`rows`) or columns beyond the last full tile that are better a product of their own, 0 if none are, and the expected time
-struct Rest {
-    int64_t count;
-    bool rows;
-    double us;
-};
-Rest rest_of(Way way, int64_t M, int64_t N, int64_t K, double whole_us, bool columns_only) {
-    Rest best{0, false, whole_us};
-    for (int64_t side : {128, 256})
-        for (bool rows : {true, false}) {
-            const int64_t all = rows ? M : N, r = all % side;
-            if ((rows && columns_only) || r == 0 || r > side / 2 || all < side) continue;
-            const int64_t m = rows ? M - r : M, n = rows ? N : N - r;
-            double us = choose(way, m, n, K).us;
-            if (rows) us = rest_of(way, m, n, K, us, true).us;
-            us += 2 + choose(way, rows ? r : M, rows ? N : r, K).us;
-            if (us < 0.9 * whole_us && us < best.us) best = Rest{r, rows, us};
-        }
-    return best;
-}
-
-// Expected time of a product as launch_product runs it
-double product_us(Way way, int64_t M, int64_t N, int64_t K) {
-    const double us = choose(way, M, N, K).us;
-    return us > 30 ? rest_of(way, M, N, K, us, false).us : us;
-}
-
-// Expected time of two products in the largest tiles in one launch, the one with the longer tiles first: units that are through with theirs
-// (some one round earlier than others) take the other one's in turn
-double two_large_us(const Choice& a, const Choice& b) {
-    const TileKind& t = kTilesAcross[0];
-    const double ta = a.steps_each * t.full + t.ends, tb = b.steps_each * t.full + t.ends;
-    const int64_t na = a.tiles_m * a.tiles_n, late = na % kCUs;
-    int64_t nb = b.tiles_m * b.tiles_n;
-    double late_at = ((na + kCUs - 1) / kCUs) * ta, early_at = (na / kCUs) * ta;
-    const int64_t rounds = std::max<int64_t>(0, nb / kCUs - 2 - (int64_t)(ta / tb));   // of all units
-    late_at += rounds * tb, early_at += rounds * tb, nb -= rounds * kCUs;
-    while (nb > 0) {
-        if (late == 0 || early_at <= late_at) early_at += tb, nb -= kCUs - late;
-        else late_at += tb, nb -= late;
-    }
-    return std::max(late ? late_at : 0, early_at);
-}
-
 ProductArgs args_of(const ProductCall& p, const Choice& ch) {
     return ProductArgs{static_cast<const char*>(p.a), static_cast<const char*>(p.b), p.a_ld, p.b_ld, p.c, p.c_ld, p.M, p.N, p.K, (int)ch.tiles_m,
                        (int)ch.tiles_n, (int)ch.steps_each, (int)ch.splits, ch.splits > 1 ? p.partial : nullptr, epilogue_of(p.ep)};
@@ -816,10 +715,7 @@ hipError_t start_two(const ProductArgs& p, const ProductArgs& q, const ColumnSum
                      : go(k_product_two<BF, AS, BS, BS2, 2, 2, 2, 2>, Shape<BF, true, false, AS, BS, 2, 2, 2, 2>());
 }
 
-Way way_of(const ProductCall& p) {
-    if (!p.bf16) return kInFp32;
-    return !p.a_ready || !p.b_ready || p.b_fp32 ? kByRegisters : p.a_along && p.b_along ? kStraightAlong : kStraightAcross;
-}
+Way way_of(const ProductCall& p) { return way_by(p.bf16, p.a_ready, p.b_ready && !p.b_fp32, p.a_along && p.b_along); }
 int64_t join_blocks(const ProductArgs& p) { return p.partial ? (p.M * ((p.N + 7) / 8) + kWave - 1) / kWave : 0; }
 
 psgd_status join(bool bf16, const ProductArgs& p, const ProductArgs& q, const ColumnSums* sums, hipStream_t stream, std::string* what) {
@@ -860,27 +756,20 @@ int64_t product_partial_bytes(bool bf16, int64_t M, int64_t N, int64_t K) {
 
 namespace {
 
-// The rows q beyond the last full tile of p, in one launch with it where p takes the tiles `ch` and q's fill no more than one round.  `done`: so it was.
-psgd_status launch_with_rest(const ProductCall& p, const Choice& ch, const ProductCall& q, bool* done, std::string* what) {
+// The rows q beyond the last full tile of p, in one launch with it
+psgd_status launch_with_rest(const ProductCall& p, const ProductCall& q, const ProductRoute& route, std::string* what) {
     typedef Shape<true, true, true, kStraight, kStraight, 2, 4, 8, 4> Large;
     typedef Shape<true, true, true, kStraight, kStraight, 2, 2, 4, 4> Small;
-    const bool large = ch.kind == 0;
-    const int64_t wide = large ? 128 : 64, steps = (q.K + 63) / 64, tm = (q.M + 63) / 64, tn = (q.N + wide - 1) / wide;
-    const int64_t splits = std::min({kCUs * (int64_t)kTilesAlong[ch.kind].at_once / (tm * tn), steps / kLeastSteps, kMostSplits});
-    *done = splits > 1 && ch.tiles_m * ch.tiles_n + tm * tn * splits <= most_groups(lanes_of(ch.kind));
-    if (!*done) return PSGD_OK;
-    const int64_t each = (steps + splits - 1) / splits;
-    const Choice small{2, (steps + each - 1) / each, each, tm, tn, 0};
-    const ProductArgs a = args_of(p, ch), b = args_of(q, small);
-    const unsigned first = (unsigned)(tm * tn * small.splits), all = first + (unsigned)(a.tiles_m * a.tiles_n);
+    const ProductArgs a = args_of(p, route.main), b = args_of(q, route.rest);
+    const unsigned first = (unsigned)(b.tiles_m * b.tiles_n * b.splits), all = first + (unsigned)(a.tiles_m * a.tiles_n);
     auto go = [&](auto k, int lds, int threads) {
         const hipError_t e = with_lds(k, lds);
         if (e != hipSuccess) return e;
         hipLaunchKernelGGL(k, dim3(all), dim3(threads), lds, p.stream, a, b, first);
         return hipGetLastError();
     };
-    const hipError_t e = large ? go(p.b_along ? k_product_and_rest<true, 2, 4, 8, 4> : k_product_and_rest<false, 2, 4, 8, 4>, Large::kLds, Large::T)
-                               : go(p.b_along ? k_product_and_rest<true, 2, 2, 4, 4> : k_product_and_rest<false, 2, 2, 4, 4>, Small::kLds, Small::T);
+    const hipError_t e = route.main.kind == 0 ? go(p.b_along ? k_product_and_rest<true, 2, 4, 8, 4> : k_product_and_rest<false, 2, 4, 8, 4>, Large::kLds, Large::T)
+                                              : go(p.b_along ? k_product_and_rest<true, 2, 2, 4, 4> : k_product_and_rest<false, 2, 2, 4, 4>, Small::kLds, Small::T);
     const psgd_status st = product_failed(e, what);
     return st != PSGD_OK ? st : join(true, b, ProductArgs{}, nullptr, p.stream, what);
 }
@@ -889,40 +778,28 @@ psgd_status launch_with_rest(const ProductCall& p, const Choice& ch, const Produ
 
 psgd_status launch_product(const ProductCall& p, std::string* what) {
     const Way way = way_of(p);
-    const Choice ch = choose(way, p.M, p.N, p.K);
-    // Rows or columns beyond the last full tile cost a row of tiles, which may be the one too many for the last round: a product of
-    // their own, in small tiles, where that is expected to be faster by a tenth.  4099 x 2048 x 8192 bf16 205 us without.
-    if (ch.us > 30) {
-        const Rest over = rest_of(way, p.M, p.N, p.K, ch.us, false);
-        const int64_t rest = over.count;
-        const bool rows = over.rows;
-        if (rest) {
-            const int64_t z = p.bf16 ? 2 : 4, zb = p.bf16 && !p.b_fp32 ? 2 : 4, zp = p.ep.bias_bf ? 2 : 4;
-            ProductCall main = p, q = p;
-            (rows ? main.M : main.N) -= rest;
-            const int64_t row = rows ? main.M : 0, col = rows ? 0 : main.N;
-            (rows ? q.M : q.N) = rest;
-            auto moved = [&](const void* at, int64_t ld, int64_t size) { return at ? static_cast<const char*>(at) + (row * ld + col) * size : nullptr; };
-            q.a = static_cast<const char*>(p.a) + (p.a_along ? row * p.a_ld : row) * z;
-            q.b = static_cast<const char*>(p.b) + (p.b_along ? col * p.b_ld : col) * zb;
-            q.c = const_cast<char*>(moved(p.c, p.c_ld, z));
-            q.ep.pre = const_cast<char*>(moved(p.ep.pre, p.ep.pre_ld, z));
-            q.ep.residual = moved(p.ep.residual, p.ep.residual_ld, z);
-            if (p.ep.bias) q.ep.bias = static_cast<const char*>(p.ep.bias) + col * zp;
-            q.ep.row0 = p.ep.row0 + row;
-            q.ep.col0 = p.ep.col0 + col;
-            if (rows && way >= kStraightAcross && p.a_along) {
-                const Choice cm = choose(way, main.M, main.N, main.K);
-                if (cm.kind < 2 && cm.splits == 1 && (cm.us <= 30 || rest_of(way, main.M, main.N, main.K, cm.us, false).count == 0)) {
-                    bool done;
-                    const psgd_status st = launch_with_rest(main, cm, q, &done, what);
-                    if (st != PSGD_OK || done) return st;
-                }
-            }
-            const psgd_status st = launch_product(main, what);
-            if (st != PSGD_OK) return st;
-            return launch_product(q, what);
-        }
+    const ProductRoute route = product_route(way, p.a_along, p.M, p.N, p.K);
+    const Choice& ch = route.whole;
+    if (route.over) {
+        const bool rows = route.rows;
+        const int64_t z = p.bf16 ? 2 : 4, zb = p.bf16 && !p.b_fp32 ? 2 : 4, zp = p.ep.bias_bf ? 2 : 4;
+        ProductCall main = p, q = p;
+        (rows ? main.M : main.N) -= route.over;
+        const int64_t row = rows ? main.M : 0, col = rows ? 0 : main.N;
+        (rows ? q.M : q.N) = route.over;
+        auto moved = [&](const void* at, int64_t ld, int64_t size) { return at ? static_cast<const char*>(at) + (row * ld + col) * size : nullptr; };
+        q.a = static_cast<const char*>(p.a) + (p.a_along ? row * p.a_ld : row) * z;
+        q.b = static_cast<const char*>(p.b) + (p.b_along ? col * p.b_ld : col) * zb;
+        q.c = const_cast<char*>(moved(p.c, p.c_ld, z));
+        q.ep.pre = const_cast<char*>(moved(p.ep.pre, p.ep.pre_ld, z));
+        q.ep.residual = moved(p.ep.residual, p.ep.residual_ld, z);
+        if (p.ep.bias) q.ep.bias = static_cast<const char*>(p.ep.bias) + col * zp;
+        q.ep.row0 = p.ep.row0 + row;
+        q.ep.col0 = p.ep.col0 + col;
+        if (route.one_launch) return launch_with_rest(main, q, route, what);
+        const psgd_status st = launch_product(main, what);
+        if (st != PSGD_OK) return st;
+        return launch_product(q, what);
     }
     const psgd_status st = product_failed(!p.bf16 ? start_by_shape<false, kFp32, kFp32>(p, ch) : way >= kStraightAcross ? start_by_shape<true, kStraight, kStraight>(p, ch)
                                           : p.b_fp32 ? start_by_shape<true, kBf16, kFp32>(p, ch) : start_by_shape<true, kBf16, kBf16>(p, ch), what);
@@ -932,44 +809,27 @@ psgd_status launch_product(const ProductCall& p, std::string* what) {
 psgd_status launch_backward_products(bool bf16, const ProductCall* x, const ProductCall* w, const ColumnSums* sums, hipStream_t stream,
                                      std::string* what) {
     if (x && w) {
-        // In one launch where both take the same tiles and neither has rows or columns over: worth a tile that is not each one's best
-        // if what that costs is less than the launch.
-        const Way vx = way_of(*x), vw = way_of(*w);
-        const bool sx = vx >= kStraightAcross, sw = vw >= kStraightAcross;
-        // Large ones where that is expected to be faster than each by itself: 4096 x 2048 x 8192, 128 tiles of twice the length, and 8192 x 2048 x
-        // 4096, 256 tiles, 241 us one after the other and 217 together
-        if (sx && sw) {
-            const Choice lx = choose(vx, x->M, x->N, x->K, 0), lw = choose(vw, w->M, w->N, w->K, 0);
-            const bool x_first = lx.steps_each >= lw.steps_each;
-            const int64_t first = (x_first ? lx : lw).tiles_m * (x_first ? lx : lw).tiles_n, all = lx.tiles_m * lx.tiles_n + lw.tiles_m * lw.tiles_n;
-            const double apart = product_us(vx, x->M, x->N, x->K) + product_us(vw, w->M, w->N, w->K);
-            if (apart > 60 && all <= most_groups(lanes_of(0)) && two_large_us(x_first ? lx : lw, x_first ? lw : lx) < 0.95 * apart) {
-                if (const psgd_status st = sum_blocks_alone(bf16, sums, stream, what); st != PSGD_OK) return st;
-                typedef Shape<true, true, false, kStraight, kStraight, 2, 4, 8, 4> S;
-                hipError_t e = with_lds(k_product_two_large, S::kLds);
-                if (e == hipSuccess) {
-                    hipLaunchKernelGGL(k_product_two_large, dim3((unsigned)all), dim3(S::T), S::kLds, stream, args_of(*x, lx), args_of(*w, lw), (unsigned)first, (int)x_first);
-                    e = hipGetLastError();
-                }
-                const psgd_status st = product_failed(e, what);
-                return st != PSGD_OK || !sums ? st : join(bf16, ProductArgs{}, ProductArgs{}, sums, stream, what);
+        const Extent ex{way_of(*x), x->M, x->N, x->K}, ew{way_of(*w), w->M, w->N, w->K};
+        const BackwardRoute route = backward_route(ex, ew, sum_blocks(sums));
+        const ProductArgs p = args_of(*x, route.x), q = args_of(*w, route.w);
+        if (route.kind == BackwardRoute::kLarge) {
+            if (const psgd_status st = sum_blocks_alone(bf16, sums, stream, what); st != PSGD_OK) return st;
+            typedef Shape<true, true, false, kStraight, kStraight, 2, 4, 8, 4> S;
+            const int64_t px = p.tiles_m * p.tiles_n, pw = q.tiles_m * q.tiles_n;
+            hipError_t e = with_lds(k_product_two_large, S::kLds);
+            if (e == hipSuccess) {
+                hipLaunchKernelGGL(k_product_two_large, dim3((unsigned)(px + pw)), dim3(S::T), S::kLds, stream, p, q, (unsigned)(route.x_first ? px : pw), (int)route.x_first);
+                e = hipGetLastError();
             }
+            const psgd_status st = product_failed(e, what);
+            return st != PSGD_OK || !sums ? st : join(bf16, ProductArgs{}, ProductArgs{}, sums, stream, what);
         }
-        Choice cx = choose(vx, x->M, x->N, x->K), cw = choose(vw, w->M, w->N, w->K);
-        if (cx.us + cw.us < 150 && (cx.kind != cw.kind || cx.kind == 0)) {
-            double least = cx.us + cw.us + 4;
-            for (int kind : {1, 2}) {
-                const Choice tx = choose(vx, x->M, x->N, x->K, kind), tw = choose(vw, w->M, w->N, w->K, kind);
-                if (tx.us + tw.us < least) least = tx.us + tw.us, cx = tx, cw = tw;
-            }
-        }
-        const int64_t blocks = cx.tiles_m * cx.tiles_n * cx.splits + cw.tiles_m * cw.tiles_n * cw.splits + sum_blocks(sums);
-        if (cx.kind == cw.kind && cx.kind > 0 && cx.us + cw.us < 150 && blocks <= most_groups(lanes_of(cx.kind))) {
-            const ProductArgs p = args_of(*x, cx), q = args_of(*w, cw);
-            const hipError_t e = !bf16 ? start_two<false, kFp32, kFp32, kFp32>(p, q, sums, cx.kind, stream)
-                                 : sx && sw ? start_two<true, kStraight, kStraight, kStraight>(p, q, sums, cx.kind, stream)
-                                 : x->b_fp32 ? start_two<true, kBf16, kFp32, kBf16>(p, q, sums, cx.kind, stream)
-                                             : start_two<true, kBf16, kBf16, kBf16>(p, q, sums, cx.kind, stream);
+        if (route.kind == BackwardRoute::kTogether) {
+            const int kind = route.x.kind;
+            const hipError_t e = !bf16 ? start_two<false, kFp32, kFp32, kFp32>(p, q, sums, kind, stream)
+                                 : ex.way >= kStraightAcross && ew.way >= kStraightAcross ? start_two<true, kStraight, kStraight, kStraight>(p, q, sums, kind, stream)
+                                 : x->b_fp32 ? start_two<true, kBf16, kFp32, kBf16>(p, q, sums, kind, stream)
+                                             : start_two<true, kBf16, kBf16, kBf16>(p, q, sums, kind, stream);
             const psgd_status st = product_failed(e, what);
             return st != PSGD_OK ? st : join(bf16, p, q, sums, stream, what);
         }
