@@ -122,8 +122,8 @@ bool lay_out(const void* src, int64_t src_ld, bool src_bf, void* dst, int64_t ds
 }
 
 // The weights or the input as operand B or A of the product q.M x q.N x q.K
-bool weights(const LinearCall& c, const Parts& p, ProductCall& q, std::string* what) {
-    const Comes w = weights_come(c);
+bool weights(const LinearCall& c, const Parts& p, ProductCall& q, bool other_ready, std::string* what) {
+    const Comes w = weights_come(c, other_ready);
     q.b = c.w;
     q.b_ld = c.k;
     q.b_fp32 = c.bf16 && !c.param_bf16 && !w.lay;
@@ -134,8 +134,8 @@ bool weights(const LinearCall& c, const Parts& p, ProductCall& q, std::string* w
     q.b_ld = p.k_ld;
     return lay_out(c.w, c.k, c.param_bf16, to, p.k_ld, c.n, c.k, q.stream, what);
 }
-bool input(const LinearCall& c, const Parts& p, const ProductCall& q, const void** x, int64_t* ld, bool* ready, std::string* what) {
-    const Comes in = input_comes(c, !q.a_along);
+bool input(const LinearCall& c, const Parts& p, const ProductCall& q, bool other_ready, const void** x, int64_t* ld, bool* ready, std::string* what) {
+    const Comes in = input_comes(c, !q.a_along, other_ready);
     *x = c.x;
     *ld = c.x_ld;
     *ready = in.ready || in.lay;
@@ -177,7 +177,8 @@ psgd_status launch_linear_forward(const LinearCall& c, std::string* what) {
     q.ep = ep;
     q.partial = reinterpret_cast<float*>(static_cast<char*>(c.workspace) + p.partial);
     q.stream = static_cast<hipStream_t>(c.stream);
-    if (!weights(c, p, q, what) || !input(c, p, q, &q.a, &q.a_ld, &q.a_ready, what)) return PSGD_EHIP;
+    const Comes w = weights_come(c, true), in = input_comes(c, false, true);   // each by itself
+    if (!weights(c, p, q, in.ready || in.lay, what) || !input(c, p, q, w.ready || w.lay, &q.a, &q.a_ld, &q.a_ready, what)) return PSGD_EHIP;
     return launch_product(q, what);
 }
 
@@ -186,20 +187,18 @@ psgd_status launch_linear_backward(const LinearCall& c, std::string* what) {
     const Parts p = parts_of(c);
     const float scale = c.drop.below ? c.drop.factor : 1.f;
     if (c.T == 0 && c.accumulate) return PSGD_OK;
-    const bool direct = c.act == PSGD_ACT_IDENTITY && !c.drop.below;   // dz is dy
+    const Comes come = dz_comes(c);
+    const bool direct = !come.lay;   // dz is read in dy's place
     char* const ws = static_cast<char*>(c.workspace);
     const int64_t blocks = up(c.T, kSumRows) / kSumRows;
     if ((!direct || c.db) && (c.n + 255) / 256 * blocks > most_groups(kBlock)) return PSGD_EUNSUPPORTED;   // before anything is launched
     const void* dz = c.dy;
     int64_t dz_ld = c.dy_ld;
-    bool dz_ready = false;
+    const bool dz_ready = come.ready || come.lay;
     if (c.T > 0) {
         if (!direct) {   // rows padded with zeros to multiples of sixteen bytes
             dz = ws + p.dz;
             dz_ld = p.n_ld;
-        }
-        dz_ready = dz_comes(c, direct).ready;
-        if (!direct) {
             auto k = c.bf16 ? k_dz<true> : k_dz<false>;
             hipLaunchKernelGGL(k, dim3((unsigned)((c.n + 255) / 256 * blocks)), dim3(kBlock), 0, s, c.dy, c.dy_ld, c.pre, c.pre_ld, c.act, drop_of(c.drop),
                                const_cast<void*>(dz), dz_ld, c.db ? reinterpret_cast<float*>(ws + p.db) : nullptr, c.T, c.n);
@@ -224,7 +223,7 @@ psgd_status launch_linear_backward(const LinearCall& c, std::string* what) {
         x.c_ld = c.dx_ld;
         x.M = c.T;
         x.K = c.n;
-        if (!weights(c, p, x, what)) return PSGD_EHIP;
+        if (!weights(c, p, x, dz_ready, what)) return PSGD_EHIP;
         w.partial += up(product_partial_bytes(c.bf16, c.T, c.k, c.n), 256) / 4;
     }
     if (c.dw) {
@@ -232,7 +231,7 @@ psgd_status launch_linear_backward(const LinearCall& c, std::string* what) {
         w.c_ld = c.k;
         w.M = c.n;
         w.K = c.T;
-        if (!input(c, p, w, &w.b, &w.b_ld, &w.b_ready, what)) return PSGD_EHIP;
+        if (!input(c, p, w, dz_ready, &w.b, &w.b_ld, &w.b_ready, what)) return PSGD_EHIP;
         if (c.accumulate) {
             w.ep.residual = c.dw;
             w.ep.residual_ld = c.k;

@@ -205,20 +205,31 @@ inline bool lay_out_pays(const LinearCall& c, int64_t rows, int64_t ld, bool wei
     return weight_gradient ? work >= 2e9 : c.T >= (c.param_bf16 ? 640 : 1000) && work >= 1e10;
 }
 
-// Which operands of a bf16 product can go straight to LDS where they are (`ready`), and which are laid out for it first (`lay`)
+// Which operands of a bf16 product can go straight to LDS where they are (`ready`), and which are laid out for it first (`lay`).  For bf16 operands that
+// is of use only if the product's other operand comes that way too; fp32 weights are rounded once instead of in every tile (the input gradient of 1500 x
+// 4095 x 2000 through registers 83 us in place, 75 laid out; of 8192 x 50257 x 2048 3208 and 2218).
 struct Comes {
     bool ready, lay;
 };
-inline Comes weights_come(const LinearCall& c) {
+inline Comes weights_come(const LinearCall& c, bool other_ready) {
     const bool ready = !c.bf16 || (c.param_bf16 && c.k % 8 == 0);
-    return Comes{ready, !ready && lay_out_pays(c, c.n, up(c.k, 8), false)};
+    return Comes{ready, !ready && (other_ready || !c.param_bf16) && lay_out_pays(c, c.n, up(c.k, 8), false)};
 }
-inline Comes input_comes(const LinearCall& c, bool weight_gradient) {
+inline Comes input_comes(const LinearCall& c, bool weight_gradient, bool other_ready) {
     const bool ready = !c.bf16 || (vec_aligned(c.x, c.x_ld) && c.k % 8 == 0);
-    return Comes{ready, !ready && lay_out_pays(c, c.T, up(c.k, 8), weight_gradient)};
+    return Comes{ready, !ready && other_ready && lay_out_pays(c, c.T, up(c.k, 8), weight_gradient)};
 }
-inline Comes dz_comes(const LinearCall& c, bool direct) {   // direct: dz is dy, otherwise written for the products with padded rows
-    return Comes{!c.bf16 || !direct || (vec_aligned(c.dy, c.dy_ld) && c.n % 8 == 0), false};
+// dz: where it is dy itself, it can be read in place; otherwise it is written for the products anyway, in padded rows.  That is done with dy too (`lay`)
+// where its rows do not begin on multiples of sixteen bytes and the products are large enough, or both go through registers.  us, in place / laid
+// out, n x k, tokens: both gradients 1001 x 1000 1500 33 / 32, with fp32 weights 35 / 40, 8192 82 / 73 and 80 / 87; 4095 x 4096 300 60 / 65, 700
+// 117 / 88, 4000 424 / 263, fp32 441 / 280; 650 x 2601 4000 80 / 97, 8192 135 / 127; 50257 x 2048 300 302 / 251, 8192 4329 / 3717, fp32 4552 /
+// 3853.  The input gradient alone: 650 x 2601 8192 62 / 66; 4095 x 4096 700 50 / 53, 1500 88 / 77.  The weight gradient alone: 1001 x 1000 300
+// 15 / 15, 700 22 / 19; 4095 x 4096 4000 242 / 133; 650 x 2601, where the input is laid out too, 1500 37 / 40, 4000 74 / 64.
+inline Comes dz_comes(const LinearCall& c) {
+    if (c.act != PSGD_ACT_IDENTITY || c.drop.below) return Comes{false, true};
+    if (!c.bf16 || (vec_aligned(c.dy, c.dy_ld) && c.n % 8 == 0)) return Comes{true, false};
+    const double work = (double)c.T * (double)c.n * (double)c.k, least = !c.dw ? 2e10 : c.dx ? 1e10 : input_comes(c, true, true).ready ? 1e9 : 4e9;
+    return Comes{false, work >= least && (c.n + 255) / 256 * ((c.T + kSumRows - 1) / kSumRows) <= most_groups(kBlock)};
 }
 
 // ---- the forward product of a few tokens ----------------------------------------------------------------------------

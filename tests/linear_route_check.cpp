@@ -46,18 +46,24 @@ int main() {
                 std::printf("few\n");
                 continue;
             }
-            const Comes w = weights_come(c), in = input_comes(c, false);
+            const Comes w0 = weights_come(c, true), in0 = input_comes(c, false, true);
+            const Comes w = weights_come(c, in0.ready || in0.lay), in = input_comes(c, false, w0.ready || w0.lay);
             if (w.lay) out += " lay:w";
             if (in.lay) out += " lay:x";
             out += product({way_by(bf16, in.ready || in.lay, w.ready || w.lay, true), true, true, w_fp32 && !w.lay}, T, n, k);
         } else {
-            const Comes dz = dz_comes(c, direct), w = weights_come(c), in = input_comes(c, true);
+            char some;
+            c.act = direct ? PSGD_ACT_IDENTITY : PSGD_ACT_GELU;
+            c.dx = pass == 'w' ? nullptr : &some;
+            c.dw = pass == 'x' ? nullptr : &some;
+            const Comes dz = dz_comes(c);
             const bool a = dz.ready || dz.lay;
-            if (dz.lay) out += " lay:dz";
+            const Comes w = weights_come(c, a), in = input_comes(c, true, a);
+            if (dz.lay && direct) out += " lay:dy";
             if (w.lay && pass != 'w') out += " lay:w";
             if (in.lay && pass != 'x') out += " lay:x";
             const Operands ox{way_by(bf16, a, w.ready || w.lay, false), true, false, w_fp32 && !w.lay}, ow{way_by(bf16, a, in.ready || in.lay, false), false, false, false};
-            const int64_t sums = direct && bias ? (n + 255) / 256 * ((T + kSumRows - 1) / kSumRows) : 0;
+            const int64_t sums = !dz.lay && bias ? (n + 255) / 256 * ((T + kSumRows - 1) / kSumRows) : 0;
             const BackwardRoute r = backward_route({ox.way, T, k, n}, {ow.way, n, k, T}, sums);
             if (pass == 'x') out += product(ox, T, k, n);
             else if (pass == 'w') out += product(ow, n, k, T);

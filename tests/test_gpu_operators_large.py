@@ -57,7 +57,7 @@ CALLS = [(p, T, n, k, *types, direct) for p, T, n, k, types, direct in [
     # both in one launch
     ("b", 2187, 1744, 2432, MIX, 0), ("b", 2187, 1744, 2432, BF, 1), ("b", 997, 1992, 4368, MIX, 0), ("b", 997, 1992, 4368, BF, 1),
     ("b", 965, 208, 4152, FP, 0), ("b", 209, 216, 72, FP, 1), ("b", 459, 209, 8317, MIX, 0), ("b", 232, 232, 72, MIX, 1),
-    ("b", 209, 3633, 1177, BF, 0), ("b", 203, 223, 43, BF, 1), ("b", 6301, 200, 664, BF, 0), ("b", 210, 248, 72, BF, 1),
+    ("b", 209, 3633, 1177, BF, 0), ("b", 203, 223, 43, BF, 1), ("b", 2187, 1745, 2700, MIX, 1), ("w", 2187, 1745, 1201, BF, 1), ("x", 2187, 4091, 2433, BF, 1), ("b", 6301, 200, 664, BF, 0), ("b", 210, 248, 72, BF, 1),
 ]] + [("f", T, n, 136, *types, direct) for T, n in ((1, 8200), (16, 8193), (20, 8208), (32, 8195)) for types in (BF, MIX, FP) for direct in (0, 1)]
 
 
