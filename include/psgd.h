@@ -334,7 +334,10 @@ PSGD_API psgd_status psgd_plan_kept(const psgd_plan* plan, int32_t tensor, int64
  *   rng     (device, const)  two 64-bit words {seed, offset}, 8-byte aligned.  Key of the generator: the seed; upper
  *                            half of its counter: the offset plus the argument `offset`.  A captured graph draws
  *                            anew on each replay if the program moves rng[1] on between the replays; calls of one
- *                            step are told apart by `offset`.  Same words, same offset: same mask.
+ *                            step are told apart by `offset`.  Only the sum rng[1] + offset counts: same seed, same sum,
+ *                            same mask.  So a step that uses the offsets 0 .. c - 1 moves rng[1] on by c at least (by 1, and
+ *                            layer i would draw what layer i + 1 drew a step before).  Dropout and the random mask count in the
+ *                            same space too: where one seed serves both, they take different offsets.
  *   p, drop                  drop probability in [0, 1], taken as the multiple d of 2^-16 next to it; the elements
  *                            that stay are multiplied by 1 / (1 - d) (with d = 1 none does).  Element (row, col) of
  *                            [rows][cols]: counter (col / 8, row), half word col % 8 of the four words (low
