@@ -379,6 +379,8 @@ typedef struct {
 /* Scratch that psgd_linear_forward and psgd_linear_backward need for this layer and token count (the larger of the
  * two; rng, drop and offset do not matter).  It does not shrink as tokens grow: that of the longest batch serves all. */
 PSGD_API psgd_status psgd_linear_workspace(const psgd_plan* plan, const psgd_linear* op, int64_t* bytes);
+/* The same for psgd_linear_forward alone, for programs that serve: no more than that, and much less where tokens are many. */
+PSGD_API psgd_status psgd_linear_forward_workspace(const psgd_plan* plan, const psgd_linear* op, int64_t* bytes);
 
 /* z = x W^T + b ; y = residual + D(act(z)).  x, residual, pre and y have the plan's grad_dtype.
  *   param    (device, const)  flat parameters, laid out like `out` of psgd_decompress, 16-byte aligned
@@ -387,7 +389,7 @@ PSGD_API psgd_status psgd_linear_workspace(const psgd_plan* plan, const psgd_lin
  *   pre      (device, out)    [tokens][n] or NULL: z, which the backward pass of an activation reads
  *   y        (device, out)    [tokens][n]; may be `residual` itself with the same stride, otherwise outputs overlap
  *                             nothing
- *   workspace (device)        psgd_linear_workspace bytes, 256-byte aligned, contents ignored and left undefined;
+ *   workspace (device)        psgd_linear_workspace or psgd_linear_forward_workspace bytes, 256-byte aligned, contents ignored and left undefined;
  *                             calls that may run at the same time need workspaces of their own
  * Errors: PSGD_EINVAL for null or misaligned pointers, tensor indices that are not such a matrix or vector, a negative
  * token count, a stride below the row length, drop outside [0, 1]; PSGD_EUNSUPPORTED for more than 2^20 rows or

@@ -109,6 +109,8 @@ def load_library(path: Optional[str] = None):
     lib.psgd_plan_read_trace.argtypes = [vp, C.POINTER(C.c_uint64), i64, C.POINTER(i64)]
     lib.psgd_linear_workspace.restype = C.c_int
     lib.psgd_linear_workspace.argtypes = [vp, C.POINTER(psgd_linear), C.POINTER(i64)]
+    lib.psgd_linear_forward_workspace.restype = C.c_int
+    lib.psgd_linear_forward_workspace.argtypes = [vp, C.POINTER(psgd_linear), C.POINTER(i64)]
     lib.psgd_linear_forward.restype = C.c_int
     lib.psgd_linear_forward.argtypes = [vp, C.POINTER(psgd_linear), vp, vp, vp, vp, vp, vp, vp]
     lib.psgd_linear_backward.restype = C.c_int
@@ -251,6 +253,12 @@ class Plan:
         n = C.c_int64()
         op = self._linear(weight, tokens, param_dtype, **op)
         self._check(self._lib.psgd_linear_workspace(self._h, C.byref(op), C.byref(n)), "psgd_linear_workspace")
+        return n.value
+
+    def linear_forward_workspace(self, weight, tokens, param_dtype=PSGD_F32, **op) -> int:
+        n = C.c_int64()
+        op = self._linear(weight, tokens, param_dtype, **op)
+        self._check(self._lib.psgd_linear_forward_workspace(self._h, C.byref(op), C.byref(n)), "psgd_linear_forward_workspace")
         return n.value
 
     def linear_forward(self, weight, tokens, param, x, y, workspace, residual=None, pre=None, param_dtype=PSGD_F32, stream=None,

@@ -99,17 +99,20 @@ struct Parts {
     int64_t k_ld, n_ld;              // row lengths of laid-out operands
 };
 
-Parts parts_of(const LinearCall& c) {
+Parts parts_of(const LinearCall& c, bool forward) {
     Parts p{};
     const int64_t z = c.bf16 ? 2 : 4;
     p.k_ld = c.bf16 ? up(c.k, 8) : c.k;
     p.n_ld = c.bf16 ? up(c.n, 8) : c.n;
     int64_t at = 0;
     auto take = [&](int64_t bytes) { const int64_t was = at; at += up(bytes, 256); return was; };
-    p.w = c.bf16 && (!c.param_bf16 || c.k % 8) ? take(c.n * p.k_ld * z) : -1;
-    p.x = c.bf16 ? take(c.T * p.k_ld * z) : 0;
-    p.dz = take(c.T * p.n_ld * z);
-    p.db = take(up(c.T, kSumRows) / kSumRows * c.n * 4);
+    const bool copies = c.bf16 && (!forward || large_enough(c, false));   // whether x is aligned is not known yet
+    p.w = copies && (!c.param_bf16 || c.k % 8) ? take(c.n * p.k_ld * z) : -1;
+    p.x = copies ? take(c.T * p.k_ld * z) : 0;
+    if (!forward) {
+        p.dz = take(c.T * p.n_ld * z);
+        p.db = take(up(c.T, kSumRows) / kSumRows * c.n * 4);
+    }
     p.partial = at;
     return p;
 }
@@ -150,8 +153,13 @@ bool input(const LinearCall& c, const Parts& p, const ProductCall& q, bool other
 
 int64_t linear_workspace_bytes(const LinearCall& c) {
     if (c.T == 0) return 0;
-    return parts_of(c).partial + std::max(product_partial_bytes(c.bf16, c.T, c.n, c.k),
+    return parts_of(c, false).partial + std::max(product_partial_bytes(c.bf16, c.T, c.n, c.k),
                                           up(product_partial_bytes(c.bf16, c.T, c.k, c.n), 256) + product_partial_bytes(c.bf16, c.n, c.k, c.T));
+}
+
+int64_t linear_forward_workspace_bytes(const LinearCall& c) {
+    if (c.T == 0) return 0;
+    return few_tokens(c) ? 256 : std::max<int64_t>(256, parts_of(c, true).partial + product_partial_bytes(c.bf16, c.T, c.n, c.k));
 }
 
 psgd_status launch_linear_forward(const LinearCall& c, std::string* what) {
@@ -165,7 +173,7 @@ psgd_status launch_linear_forward(const LinearCall& c, std::string* what) {
     ep.residual_ld = c.residual_ld;
     ep.drop = c.drop;
     if (few_tokens(c)) return launch_few_tokens(c, ep, what);
-    const Parts p = parts_of(c);
+    const Parts p = parts_of(c, true);
     ProductCall q{};
     q.bf16 = c.bf16;
     q.a_along = q.b_along = true;
@@ -184,7 +192,7 @@ psgd_status launch_linear_forward(const LinearCall& c, std::string* what) {
 
 psgd_status launch_linear_backward(const LinearCall& c, std::string* what) {
     const hipStream_t s = static_cast<hipStream_t>(c.stream);
-    const Parts p = parts_of(c);
+    const Parts p = parts_of(c, false);
     const float scale = c.drop.below ? c.drop.factor : 1.f;
     if (c.T == 0 && c.accumulate) return PSGD_OK;
     const Comes come = dz_comes(c);

@@ -199,10 +199,12 @@ inline Way way_by(bool bf16, bool a_ready, bool b_ready, bool along) {
 // 119 / 165; 50304 x 2048 700 270 / 229, 1500 380 / 444; 4096 x 4095 bf16, both operands, 300 48 / 41, 700 54 / 68, 4000 124 / 196; 2600 x 650
 // bf16 1500 25 / 16, 4000 39 / 32.  The weight gradient, which reads the input alone in another place: 1000 x 1001, 4000 tokens 34 / 31, 2600 x
 // 650 700 14 / 13, 1500 23 / 25, 4000 47 / 64; 4096 x 4095 300 30 / 31, 4000 121 / 192.
-inline bool lay_out_pays(const LinearCall& c, int64_t rows, int64_t ld, bool weight_gradient) {
-    if ((rows * (ld / 8) + kBlock - 1) / kBlock > most_groups(kBlock)) return false;   // more than one launch takes: 64 GiB
+inline bool large_enough(const LinearCall& c, bool weight_gradient) {
     const double work = (double)c.T * (double)c.n * (double)c.k;
     return weight_gradient ? work >= 2e9 : c.T >= (c.param_bf16 ? 640 : 1000) && work >= 1e10;
+}
+inline bool lay_out_pays(const LinearCall& c, int64_t rows, int64_t ld, bool weight_gradient) {
+    return large_enough(c, weight_gradient) && (rows * (ld / 8) + kBlock - 1) / kBlock <= most_groups(kBlock);   // one launch takes 64 GiB
 }
 
 // Which operands of a bf16 product can go straight to LDS where they are (`ready`), and which are laid out for it first (`lay`).  For bf16 operands that

@@ -77,6 +77,15 @@ psgd_status psgd_linear_workspace(const psgd_plan* plan, const psgd_linear* op, 
     return PSGD_OK;
 }
 
+psgd_status psgd_linear_forward_workspace(const psgd_plan* plan, const psgd_linear* op, int64_t* bytes) {
+    if (!bytes) return PSGD_EINVAL;
+    LinearCall c{};
+    psgd_status st = linear_args(plan, op, &c);
+    if (st != PSGD_OK) return st;
+    *bytes = psgd::linear_forward_workspace_bytes(c);
+    return PSGD_OK;
+}
+
 psgd_status psgd_linear_forward(psgd_plan* plan, const psgd_linear* op, const void* param, const void* x, const void* residual,
                                 void* pre, void* y, void* workspace, void* hip_stream) try {
     LinearCall c{};

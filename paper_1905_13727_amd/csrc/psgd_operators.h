@@ -66,6 +66,7 @@ struct DropoutCall {
 };
 
 int64_t linear_workspace_bytes(const LinearCall& c);
+int64_t linear_forward_workspace_bytes(const LinearCall& c);   // no more than that
 // *what: the launch that failed and HIP's text, where the status is PSGD_EHIP
 psgd_status launch_linear_forward(const LinearCall& c, std::string* what);
 psgd_status launch_linear_backward(const LinearCall& c, std::string* what);
