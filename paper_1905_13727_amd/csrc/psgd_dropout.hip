@@ -90,7 +90,8 @@ __device__ __forceinline__ void st_out4(void* p, int64_t at, v4f v) {
 // something read theirs again.  STREAM: the error memory goes around the caches, where the plan says that all workers' is larger than
 // they are: fp32, ResNet18-shaped, 16 workers 438 us without, 411 with; transformer of 4 layers, bf16, 590 and 568; 4 workers of the
 // first set 88 and 98.
-// Memory bounds it: 5.3 and 6.4 TB/s there of 4 W + 8 W + 4 bytes an element; one call of the generator for four entries is hidden.
+// Memory bounds it: 5.3 and 6.5 TB/s there of 4 W + 8 W + 4 bytes an element; one call of the generator for four entries is hidden.  Beyond 16 workers the
+// second walk shows: the first set, 17 workers 513 us, 32 1026, 64 2240, 4.5 to 3.9 TB/s of the same bytes.
 template <bool GBF, bool OBF, int CAP, bool STREAM>
 __global__ __launch_bounds__(kBlock) void k_random_mask(const MatDesc* __restrict__ mats, const int64_t* __restrict__ first, int n_mats,
                                                         const void* __restrict__ grad, float* __restrict__ err, void* __restrict__ out,

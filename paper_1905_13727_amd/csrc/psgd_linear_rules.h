@@ -239,7 +239,7 @@ inline Comes dz_comes(const LinearCall& c) {
 // At most kFewTokens tokens, without scratch and whatever the operands' types and alignment.
 constexpr int64_t kFewTokens = 32;
 // Where this takes less time than the tiles of the other products, which read x once for 64 rows of W and divide the contraction
-// over the chip: us, this / tiles, one, 16 and 32 tokens, n x k.
+// over the chip: us, this / tiles, one, 16 and 32 tokens, n x k, called again and again, so that weights of up to some 200 MB come from the caches.
 //   fp32: 650 x 650 4.3 / 9.7, 4.6 / 9.8, 6.4 / 10.1; 8192 x 2048 12.9 / 24.9, 16.9 / 25.3, 18.4 / 26.2; 50304 x 2048 82 / 137, 107 / 137, 119 / 138;
 //   2048 x 8192, short of workgroups, 20.5 / 25.9, 30.4 / 26.3, 44.5 / 26.8; 512 x 8192 19.6 / 13.3.
 //   bf16: 512 x 512 2.9 / 4.6, 3.3 / 4.7, 3.7 / 5.0; 2048 x 2048 4.4 / 6.6, 5.8 / 7.0, 7.5 / 7.6; 8192 x 2048 6.6 / 9.9, 7.9 / 16.1, 9.8 / 16.6; beyond
@@ -248,6 +248,11 @@ constexpr int64_t kFewTokens = 32;
 //   4095 18.7 / 11.5, 30.3 / 13.0, 43.4 / 13.7.
 //   bf16, fp32 weights: 512 x 512 3.4 / 6.0, 4.1 / 6.0, 5.0 / 6.5; 1000 x 1001 4.8 / 7.4, 6.6 / 8.0, 9.4 / 8.2; 2048 x 2048 6.9 / 7.5, 9.5 / 8.0, 13.0 / 8.6;
 //   8192 x 2048 12.5 / 15.1, 16.8 / 15.9, 18.9 / 16.6; 50304 x 2048 69 / 103, 97 / 105, 109 / 108.
+// With the weights from memory, as a model of more layers than the caches hold reads them, both take longer and this one loses later: fp32 8192 x 2048 16.1 /
+// 26.8, 19.7 / 27.2, 19.7 / 27.8; 2048 x 8192 25.9 / 28.3, 31.6 / 29.3, 48.1 / 29.7; bf16 2048 x 2048 5.2 / 9.4, 6.6 / 10.2, 9.2 / 11.0; 8192 x 2048 9.6 / 13.6,
+// 10.6 / 25.3, 12.4 / 25.6; 8192 x 4096 18.7 / 19.3, 19.3 / 19.9, 21.9 / 20.7; 50304 x 2048 41.4 / 48.8, 54.7 / 49.4, 66.4 / 51.5; 2048 x 8192 13.7 / 14.2, 17.5
+// / 14.6, 27.3 / 15.1; bf16, fp32 weights 8192 x 2048 14.1 / 17.6, 17.8 / 18.0, 19.9 / 19.1; 50304 x 2048 70.1 / 99.0, 99.1 / 100.5, 111.1 / 102.6; and on
+// the other side of the lines on n, small layers with a longer contraction: fp32 158 x 700 4.4 / 10.2 for one token.
 inline bool few_tokens(const LinearCall& c) {
     if (c.T > kFewTokens) return false;
     const int64_t weights = c.n * c.k;

@@ -9,6 +9,9 @@
 //   along    chunk c of row r lies at place c ^ (r & 7) of its eight;
 //   across   row l of the contraction holds its chunks in the order c ^ f(l), f such that the four rows of a transposing read
 //            (ds_read_b64_tr_b16: four rows of the contraction, sixteen of the output) lie in different banks.
+// No conflict is counted along the contraction, nor across it in bf16 tiles of 128 and 256.  Across it two cases do meet banks twice: a bf16 tile of 64
+// has eight chunks a row, too few for all of f (both operands across, 2048 cubed: 4.3e6 of 8.7e6 active LDS cycles), and fp32 rows are not permuted
+// (1.7e7 of 4.2e7, of 8.1e7 that the units were busy, and the product takes 1 % longer than the one along / along, whose conflicts are 6.6e4).
 // Operands that cannot be loaded that way go through registers instead: fp32 ones (their matrix instructions leave time enough,
 // and a row may then begin at any element), bf16 ones whose rows do not begin on multiples of sixteen bytes, and fp32 weights
 // rounded to bf16 on the way.
@@ -536,8 +539,8 @@ __global__ __launch_bounds__(WM* WN* kWave, 2) void k_product(ProductArgs p) {
 }
 
 // A product p and, in front of it in the same launch, the rows q beyond its last full tile in tiles of 64 rows, divided along the contraction so that
-// each unit has one more short tile.  bf16, in two launches and so: 4099 x 8192 x 2048 122 and 115 us, 4099 x 2048 x 2048 41.5 and 38.8, 4099 x 2048 x
-// 8192 127 and 126.
+// each unit has one more short tile.  bf16, in two launches and so: 4099 x 8192 x 2048 124 and 115 us, 4099 x 2048 x 2048 40.3 and 37.7; with a long
+// contraction it gains nothing, 4099 x 2048 x 8192 131 and 132, with dropout and residual 139 and 139 (188 as one product).
 template <bool BA, int WM, int WN, int MF, int NF>
 __global__ __launch_bounds__(WM* WN* kWave, 2) void k_product_and_rest(ProductArgs p, ProductArgs q, unsigned first) {
     extern __shared__ __attribute__((aligned(16))) char lds_raw[];
