@@ -175,3 +175,62 @@ def test_the_largest_tiles_in_a_graph(T, n, k):
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(eager, replayed))
         assert bool(torch.isfinite(eager[3]).all()) and float(eager[3].abs().max()) > 0
+
+
+@pytest.mark.parametrize("which,T,n,k,dtype,params,direct", [c for c in CALLS if c[0] == "f" and not c[-1]])
+def test_adding_to_the_residual_in_place(which, T, n, k, dtype, params, direct):
+    """y is the residual itself, whichever launches a call is: the same bits as into another buffer."""
+    dev = _need_gpu()
+    L = Layer(n, k, dtype, params, dev)
+    gen = torch.Generator(device=dev).manual_seed(n)
+    x, res, ws = _noise(L, gen, T, k), _noise(L, gen, T, n), L.workspace(T)
+    y, z = torch.empty_like(res), res.clone()
+    for to, add in ((y, res), (z, z)):
+        L.plan.linear_forward(1, T, L.param, x, to, ws, residual=add, activation="silu", drop=0.25, rng=_rng(dev), **L.op())
+    assert torch.equal(y, z)
+
+
+@pytest.mark.parametrize("T,n,k,dtype,params", [(20, 8208, 136, "bf16", "f32"), (66, 72, 1736, "bf16", "bf16"), (997, 1992, 4368, "bf16", "bf16"),
+                                               (700, 2600, 650, "f32", "f32"), (2187, 1745, 1201, "bf16", "f32")])
+def test_calls_at_the_same_time(T, n, k, dtype, params):
+    """Two streams with a workspace each, over one plan and one set of parameters, and two graphs that share a workspace, replayed in turn: the
+    bits of the same calls one after the other."""
+    dev = _need_gpu()
+    L = Layer(n, k, dtype, params, dev)
+    gen = torch.Generator(device=dev).manual_seed(k)
+    op = {name: v for name, v in L.op().items() if name != "stream"}
+    sets = [dict(x=_noise(L, gen, T, k), dy=_noise(L, gen, T, n), ws=L.workspace(T), worker=w) for w in range(2)]
+
+    def run(s, out, ws):
+        st = torch.cuda.current_stream().cuda_stream
+        L.plan.linear_forward(1, T, L.param, s["x"], out["y"], ws, pre=out["pre"], activation="gelu", drop=0.25, rng=rng, offset=s["worker"], stream=st, **op)
+        L.plan.linear_backward(1, T, L.param, s["x"], s["dy"], out["dx"], grad[out["name"]], ws, pre=out["pre"], worker=s["worker"], activation="gelu", drop=0.25,
+                               rng=rng, offset=s["worker"], stream=st, **op)
+        L.plan.linear_backward(1, T, L.param, s["x"], s["dy"], out["dx2"], None, ws, worker=s["worker"], stream=st, **op)
+
+    rng, dt = _rng(dev), DT[dtype]
+    grad = {name: torch.zeros(2, L.plan.sizes.grad_stride, dtype=dt, device=dev) for name in ("one", "streams", "graphs")}
+    outs = {name: [dict(name=name, y=torch.zeros(T, n, dtype=dt, device=dev), pre=torch.zeros(T, n, dtype=dt, device=dev), dx=torch.zeros(T, k, dtype=dt, device=dev),
+                        dx2=torch.zeros(T, k, dtype=dt, device=dev)) for _ in range(2)] for name in grad}
+    for s, out in zip(sets, outs["one"]):
+        run(s, out, s["ws"])
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(dev) for _ in range(2)]
+    for _ in range(5):
+        for st, s, out in zip(streams, sets, outs["streams"]):
+            with torch.cuda.stream(st):
+                run(s, out, s["ws"])
+    torch.cuda.synchronize()
+    graphs = []
+    for s, out in zip(sets, outs["graphs"]):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            run(s, out, sets[0]["ws"])
+    for _ in range(3):
+        for g in graphs:
+            g.replay()
+        torch.randn(1000, device=dev).sum().item()
+    torch.cuda.synchronize()
+    for name in ("streams", "graphs"):
+        assert torch.equal(grad["one"], grad[name])
+        assert all(torch.equal(a[f], b[f]) for a, b in zip(outs["one"], outs[name]) for f in ("y", "pre", "dx", "dx2"))
