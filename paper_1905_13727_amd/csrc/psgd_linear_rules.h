@@ -222,7 +222,7 @@ inline Comes input_comes(const LinearCall& c, bool weight_gradient, bool other_r
     return Comes{ready, !ready && other_ready && lay_out_pays(c, c.T, up(c.k, 8), weight_gradient)};
 }
 // dz: where it is dy itself, it can be read in place; otherwise it is written for the products anyway, in padded rows.  That is done with dy too (`lay`)
-// where its rows do not begin on multiples of sixteen bytes and the products are large enough, or both go through registers.  us, in place / laid
+// where its rows do not begin on multiples of sixteen bytes and the products are large enough; in place, its products go through registers.  us, in place / laid
 // out, n x k, tokens: both gradients 1001 x 1000 1500 33 / 32, with fp32 weights 35 / 40, 8192 82 / 73 and 80 / 87; 4095 x 4096 300 60 / 65, 700
 // 117 / 88, 4000 424 / 263, fp32 441 / 280; 650 x 2601 4000 80 / 97, 8192 135 / 127; 50257 x 2048 300 302 / 251, 8192 4329 / 3717, fp32 4552 /
 // 3853.  The input gradient alone: 650 x 2601 8192 62 / 66; 4095 x 4096 700 50 / 53, 1500 88 / 77.  The weight gradient alone: 1001 x 1000 300
